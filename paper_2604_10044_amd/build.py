@@ -20,7 +20,9 @@ LIB = os.path.join(PKG, "liblg.so")
 # (source, extra flags); lg_attend.hip is compiled in parts, in parallel
 ATTEND_PARTS = 7
 SOURCES = ([("lg_attend.hip", ("-DLG_ATTEND_PART=%d" % i,)) for i in range(ATTEND_PARTS)] +
-           [(s, ()) for s in ("lg_detect.hip", "lg_prune.hip", "lg_capi.hip", "lg_copy.hip")])
+           [(s, ()) for s in ("lg_detect.hip", "lg_prune.hip", "lg_capi.hip", "lg_copy.hip",
+                            "lg_rope.hip", "lg_pages.hip", "lg_paged_attend.hip",
+                            "lg_paged_capi.hip")])
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",

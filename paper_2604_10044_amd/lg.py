@@ -1,7 +1,8 @@
-"""Python binding of liblg (the C ABI in include/lg.h): argument marshalling only.
+"""Python binding of liblg (the C ABI in include/lg.h and include/lg_paged.h): argument marshalling only.
 
 Every function here has the name of the C entry point it calls and takes torch tensors (device
-memory) in place of raw pointers. Importing this module loads liblg.so and raises if it is
+memory) in place of raw pointers; those of the paged cache check the tensors' types, sizes, layout and
+device first, which the C side cannot see. Importing this module loads liblg.so and raises if it is
 missing: there is no fallback path.
 """
 from __future__ import annotations
@@ -27,6 +28,7 @@ FORM_AUTO, FORM_PORTABLE, FORM_MERGE, FORM_ONE_LAUNCH = 0, 1, 2, 3
 TEST_FORCE_HANDOVER, TEST_NO_WAIT, TEST_WHOLE_DIMS = 1, 2, 4
 LG_MODE_FULL, LG_MODE_ALWAYS_ON, LG_MODE_P1_ONLY = 0, 1, 2
 LG_POLICY_LOOPGUARD, LG_POLICY_H2O, LG_POLICY_STREAMING = 0, 1, 2
+LG_ROPE_PLAIN, LG_ROPE_LINEAR, LG_ROPE_BASE, LG_ROPE_RAMP, LG_ROPE_BANDS = 0, 1, 2, 3, 4
 STATUS = {0: "LG_OK", 1: "LG_ERR_NULL", 2: "LG_ERR_SHAPE", 3: "LG_ERR_UNSUPPORTED",
           4: "LG_ERR_PARAM", 5: "LG_ERR_WORKSPACE", 6: "LG_ERR_HIP", 7: "LG_ERR_ALIGN",
           8: "LG_ERR_TOO_LARGE"}
@@ -67,7 +69,28 @@ class GuardParams(ctypes.Structure):
         return d
 
 
-_vp, _i32, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+class PageMap(ctypes.Structure):
+    """lg_page_map; made by page_map(), which keeps the tensors alive in `tensors`."""
+    _fields_ = [("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("table", ctypes.c_void_p), ("pos", ctypes.c_void_p),
+                ("len", ctypes.c_void_p), ("ref", ctypes.c_void_p)]
+
+
+class PagedLayer(ctypes.Structure):
+    """lg_paged_layer; made by paged_layer(), which keeps the tensors alive in `tensors`."""
+    _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
+                ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p)]
+
+
+class RopeParams(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("theta", ctypes.c_double),
+                ("factor", ctypes.c_double), ("original_context", ctypes.c_double),
+                ("slow", ctypes.c_double), ("fast", ctypes.c_double)]
+
+
+_vp, _i32, _i64, _sz = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
 _lib.lg_guard_params_default.restype = GuardParams
 _lib.lg_guard_params_default.argtypes = []
 _lib.lg_status_string.restype = ctypes.c_char_p
@@ -101,6 +124,25 @@ _lib.lg_detect_and_prune.restype = ctypes.c_int
 _lib.lg_detect_and_prune.argtypes = [ctypes.POINTER(GuardParams), _i32, _vp, _i32, _vp, _vp, _vp,
                                      _vp, _vp, _i32, _i32, ctypes.POINTER(LayerCache), _vp, _vp,
                                      _vp, _vp, _vp, _vp, _vp]
+_MP, _PP = ctypes.POINTER(PageMap), ctypes.POINTER(PagedLayer)
+_lib.lg_page_workspace.restype = _sz
+_lib.lg_page_workspace.argtypes = [_MP]
+_lib.lg_page_reserve.restype = ctypes.c_int
+_lib.lg_page_reserve.argtypes = [_MP, _i32, _PP, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.lg_page_fork.restype = ctypes.c_int
+_lib.lg_page_fork.argtypes = [_MP, _vp, _vp, _sz, _vp]
+_lib.lg_page_compact.restype = ctypes.c_int
+_lib.lg_page_compact.argtypes = [_MP, _i32, _PP, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.lg_rope_frequencies.restype = ctypes.c_int
+_lib.lg_rope_frequencies.argtypes = [ctypes.POINTER(RopeParams), _vp, ctypes.POINTER(ctypes.c_float)]
+_lib.lg_rope_append.restype = ctypes.c_int
+_lib.lg_rope_append.argtypes = [_PP, _MP, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _i32, ctypes.c_float, _vp,
+                                _vp, _vp, _i32, _vp]
+_lib.lg_paged_attend_workspace.restype = _sz
+_lib.lg_paged_attend_workspace.argtypes = [_PP, _MP, _i32, _i32]
+_lib.lg_paged_attend.restype = ctypes.c_int
+_lib.lg_paged_attend.argtypes = [_PP, _MP, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _sz,
+                                 _vp]
 _lib.lg_copy_bandwidth.restype = ctypes.c_int
 _lib.lg_copy_bandwidth.argtypes = [_vp, _vp, _sz, _vp]
 
@@ -255,6 +297,159 @@ def lg_detect_and_prune(params: GuardParams, tokens, ring: int, t, t0, conf, sta
 def lg_copy_bandwidth(src, dst, nbytes: int, stream=None):
     _check(_lib.lg_copy_bandwidth(_ptr(src), _ptr(dst), nbytes, _stream(stream)),
            "lg_copy_bandwidth")
+
+
+# ------------------------------------------------------------------------------------------------
+# The paged cache (include/lg_paged.h).
+# ------------------------------------------------------------------------------------------------
+def _need(x, dtype, n, device, what):
+    """Refuses a tensor that is not dense, of this type, on this device and of at least n values."""
+    if x.dtype is not dtype or x.numel() < n or not x.is_contiguous() or x.get_device() != device:
+        raise LGError("%s: needs a contiguous %s tensor of %d values on device %d, got %s %s on %s" %
+                      (what, dtype, n, device, x.dtype, tuple(x.shape), x.device))
+    return x.data_ptr()
+
+
+def _on(device: int, layer=None):
+    """The paged calls run on the current device, which has to be the map's and the layer's."""
+    if layer is not None and layer.device != device:
+        raise LGError("the layer's pages are on device %d, the page map on device %d" % (layer.device, device))
+    if torch.cuda.current_device() != device:
+        raise LGError("the page map is on device %d, the current device is %d" %
+                      (device, torch.cuda.current_device()))
+
+
+def _bytes(workspace, device, what):
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise LGError("%s: needs a contiguous workspace on device %d" % (what, device))
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def page_map(table: torch.Tensor, pos: torch.Tensor, len_: torch.Tensor, ref: torch.Tensor,
+             page_size: int) -> PageMap:
+    """The map of a paged cache: int32 table [B][P], pos [B][P * page_size], len [B], ref [n_pages]."""
+    B, P = table.shape
+    dev = table.get_device()
+    if dev < 0:
+        raise LGError("page_map: needs device tensors")
+    m = PageMap(B, P, ref.numel(), page_size, _need(table, torch.int32, B * P, dev, "table"),
+                _need(pos, torch.int32, B * P * page_size, dev, "pos"),
+                _need(len_, torch.int32, B, dev, "len"), _need(ref, torch.int32, 1, dev, "ref"))
+    m.tensors, m.device = (table, pos, len_, ref), dev
+    return m
+
+
+def paged_layer(k: torch.Tensor, v: torch.Tensor, n_q_heads: int) -> PagedLayer:
+    """View of one layer's pages: k, v [n_pages][Hkv][page_size][D] (float32 or bfloat16)."""
+    n, Hkv, ps, D = k.shape
+    if k.dtype not in (torch.float32, torch.bfloat16) or v.shape != k.shape:
+        raise LGError("paged_layer: needs k and v of one shape, float32 or bfloat16")
+    dev = k.get_device()
+    if dev < 0:
+        raise LGError("paged_layer: needs device tensors")
+    l = PagedLayer(n, ps, n_q_heads, Hkv, D, LG_BF16 if k.dtype == torch.bfloat16 else LG_F32,
+                   _need(k, k.dtype, 1, dev, "k"), _need(v, k.dtype, 1, dev, "v"))
+    l.tensors, l.device, l.torch_dtype = (k, v), dev, k.dtype
+    return l
+
+
+def _layers(layers: Sequence[PagedLayer], device):
+    for l in layers:
+        if l.device != device:
+            raise LGError("a layer's pages are on device %d, the page map on device %d" % (l.device, device))
+    return (PagedLayer * len(layers))(*layers) if layers else None
+
+
+def lg_page_workspace(m: PageMap) -> int:
+    return int(_lib.lg_page_workspace(ctypes.byref(m)))
+
+
+def lg_page_reserve(m: PageMap, layers: Sequence[PagedLayer], q_start, t, base, workspace, stream=None):
+    dev, B, i32 = m.device, m.batch, torch.int32
+    _on(dev)
+    ws, size = _bytes(workspace, dev, "workspace")
+    _check(_lib.lg_page_reserve(ctypes.byref(m), len(layers), _layers(layers, dev),
+                                _need(q_start, i32, B + 1, dev, "q_start"), _need(t, i32, B, dev, "t"),
+                                _need(base, i32, B, dev, "base"), ws, size, _stream(stream)),
+           "lg_page_reserve")
+
+
+def lg_page_fork(m: PageMap, parent, workspace, stream=None):
+    _on(m.device)
+    ws, size = _bytes(workspace, m.device, "workspace")
+    _check(_lib.lg_page_fork(ctypes.byref(m), _need(parent, torch.int32, m.batch, m.device, "parent"),
+                             ws, size, _stream(stream)), "lg_page_fork")
+
+
+def lg_page_compact(m: PageMap, layers: Sequence[PagedLayer], keep_idx, new_len, moved, workspace, stream=None):
+    dev, B, i32 = m.device, m.batch, torch.int32
+    _on(dev)
+    ws, size = _bytes(workspace, dev, "workspace")
+    _check(_lib.lg_page_compact(ctypes.byref(m), len(layers), _layers(layers, dev),
+                                _need(keep_idx, i32, B * m.max_pages * m.page_size, dev, "keep_idx"),
+                                _need(new_len, i32, B, dev, "new_len"), _need(moved, i32, B, dev, "moved"),
+                                ws, size, _stream(stream)), "lg_page_compact")
+
+
+def lg_rope_frequencies(params: RopeParams):
+    """(inv_freq, scale): the frequencies as a float32 tensor on the host and the factor of cos and sin."""
+    inv = torch.zeros(max(1, params.rot_dim // 2), dtype=torch.float32)
+    scale = ctypes.c_float()
+    _check(_lib.lg_rope_frequencies(ctypes.byref(params), inv.data_ptr(), ctypes.byref(scale)),
+           "lg_rope_frequencies")
+    return inv, scale.value
+
+
+def _rows(x, heads, D, dtype, device, what):
+    """(pointer, row stride) of x [total][heads][D], whose rows may lie apart."""
+    if x.dtype is not dtype or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != D or \
+            x.stride(2) != 1 or x.stride(1) != D or x.get_device() != device:
+        raise LGError("%s: needs a %s tensor [rows][%d][%d] on device %d with dense heads, got %s %s on %s" %
+                      (what, dtype, heads, D, device, x.dtype, tuple(x.shape), x.device))
+    return x.data_ptr(), (x.stride(0) if x.shape[0] > 1 else heads * D)
+
+
+def lg_rope_append(layer: PagedLayer, m: PageMap, q, k, v, inv_freq, rot_dim: int, interleaved, scale: float,
+                   q_out, q_start, base, stream=None):
+    dev, D, dt, i32 = m.device, layer.head_dim, layer.torch_dtype, torch.int32
+    _on(dev, layer)
+    total = q.shape[0]
+    qp, qs = _rows(q, layer.n_q_heads, D, dt, dev, "q")
+    kp = vp = None
+    ks = vs = 0
+    if k is not None or v is not None:
+        if k is None or v is None or k.shape[0] != total or v.shape[0] != total:
+            raise LGError("lg_rope_append: needs k and v of as many rows as q, or neither")
+        kp, ks = _rows(k, layer.n_kv_heads, D, dt, dev, "k")
+        vp, vs = _rows(v, layer.n_kv_heads, D, dt, dev, "v")
+    fp = None if rot_dim == 0 else _need(inv_freq, torch.float32, rot_dim // 2, dev, "inv_freq")
+    _check(_lib.lg_rope_append(ctypes.byref(layer), ctypes.byref(m), qp, qs, kp, ks, vp, vs, fp, rot_dim,
+                               int(bool(interleaved)), scale,
+                               _need(q_out, dt, total * layer.n_q_heads * D, dev, "q_out"),
+                               _need(q_start, i32, m.batch + 1, dev, "q_start"),
+                               _need(base, i32, m.batch, dev, "base"), total, _stream(stream)),
+           "lg_rope_append")
+
+
+def lg_paged_attend_workspace(layer: PagedLayer, m: PageMap, total: int, max_chunk: int) -> int:
+    return int(_lib.lg_paged_attend_workspace(ctypes.byref(layer), ctypes.byref(m), total, max_chunk))
+
+
+def lg_paged_attend(layer: PagedLayer, m: PageMap, q, out, q_start, base, max_chunk: int, window: int,
+                    n_sink: int, suffix_w, lse, suffix_mass, conf, workspace, stream=None):
+    dev, B, dt, i32, f32 = m.device, m.batch, layer.torch_dtype, torch.int32, torch.float32
+    _on(dev, layer)
+    total, n = q.shape[0], q.shape[0] * layer.n_q_heads
+    ws, size = _bytes(workspace, dev, "workspace")
+    _check(_lib.lg_paged_attend(
+        ctypes.byref(layer), ctypes.byref(m), _need(q, dt, n * layer.head_dim, dev, "q"),
+        _need(out, dt, n * layer.head_dim, dev, "out"), _need(q_start, i32, B + 1, dev, "q_start"),
+        _need(base, i32, B, dev, "base"), total, max_chunk, window, n_sink,
+        None if suffix_w is None else _need(suffix_w, i32, B, dev, "suffix_w"),
+        _need(lse, f32, n, dev, "lse"),
+        None if suffix_mass is None else _need(suffix_mass, f32, n, dev, "suffix_mass"),
+        None if conf is None else _need(conf, f32, B, dev, "conf"), ws, size, _stream(stream)),
+        "lg_paged_attend")
 
 
 def params_from_dict(d) -> GuardParams:
