@@ -42,6 +42,7 @@ constexpr int kPagedThreads = 256;
 // Workgroups a launch aims for by splitting slots: two a CU.
 constexpr long kPagedTarget = 512;
 constexpr int kMinSplitSlots = 256;  // slots of a split at least (by capacity)
+constexpr float kSlack = 8.f;  // see paged_body
 constexpr int kHidden = 0x7fffffff;  // position of a slot whose page is missing
 
 struct PagedAttendArgs {
@@ -55,38 +56,62 @@ struct PagedAttendArgs {
   float scale_log2;
 };
 
-template <typename T, int D>
-struct Tile {
+// Sizes of the team that shares a tile: the workgroup (KW = 1) or a wave (KW = 4).
+//
+// A row of K or V in LDS is its 16-byte pieces in the order piece ^ f(row): the 16 rows whose pieces one read
+// of K takes, and the 4 rows (of 64 bytes) that a transposed read of V takes, then lie in different banks,
+// without padding. The rows a lane reads differ from its first one by multiples that leave f as it is, so the
+// exchange is one xor with a constant on its first address.
+template <typename T, int D, int KW>
+struct Team {
   static constexpr bool kF32 = sizeof(T) == 4;
   static constexpr int kRowBytes = D * (int)sizeof(T);
-  // Row strides in LDS: the 16-byte pieces of K that a read takes from 16 rows, and the 32-byte pieces
-  // (4 lanes x 8 bytes) of V that a transposed read takes from 8 rows, fall into different banks.
-  static constexpr int kStrideK = kRowBytes + 16;
-  static constexpr int kStrideV = kRowBytes + (kF32 ? 32 : 64);
-};
-
-// Sizes of the team that shares a tile: the workgroup (KW = 1) or a wave (KW = 4).
-template <typename T, int D, int KW>
-struct Team : Tile<T, D> {
-  using B = Tile<T, D>;
-  static constexpr int kKeys = B::kF32 || KW > 1 ? 32 : 64;  // slots of a tile
+  static constexpr int kRowPieces = kRowBytes / 16;
+  static constexpr int kKeys = kF32 || KW > 1 ? 32 : 64;  // slots of a tile
   static constexpr int kThreads = KW > 1 ? 64 : kPagedThreads;
-  static constexpr int kPieces = kKeys * B::kRowBytes / 16 / kThreads;  // 16-byte pieces a thread, of K and of V
-  static constexpr int kRowsStep = kThreads * 16 / B::kRowBytes;         // rows between a thread's pieces
-  static constexpr int kLdsK = kKeys * B::kStrideK, kLdsV = kKeys * B::kStrideV;
-  static constexpr int kLds = kLdsK + kLdsV + 4 * kKeys;
+  static constexpr int kPieces = kKeys * kRowPieces / kThreads;  // 16-byte pieces a thread, of K and of V
+  static constexpr int kLoadRows = 64 / kRowPieces;               // rows that a wave loads at once
+  static constexpr int kWaveLoad = kKeys / (KW > 1 ? 1 : 4);      // rows of a tile that a wave loads
+  static constexpr int kGroups = kWaveLoad > 16 ? kWaveLoad / 16 : 1;  // of 16 rows, each inside one page
+  static constexpr int kTile = kKeys * kRowBytes;
+  static constexpr int kBuffers = KW > 1 ? 1 : 2;
   // the join of KW = 4: a wave's O as [row][D + 4] and its m, l, suffix sums
-  static constexpr int kLdsJoin = KW > 1 ? kWaveRows * (D + 4) * 4 + 3 * kWaveRows * 4 : 0;
-  static constexpr int kLdsTeam = (kLds > kLdsJoin ? kLds : kLdsJoin) + 15 & ~15;
+  static constexpr int kJoin = KW > 1 ? kWaveRows * (D + 4) * 4 + 3 * kWaveRows * 4 : 0;
+  static constexpr int kLds = 2 * kTile * kBuffers > kJoin ? 2 * kTile * kBuffers : (kJoin + 511) & ~511;
+  static __device__ __forceinline__ int fk(int row) { return kF32 || D == 128 ? row & 15 : (row >> 1) & 7; }
+  static __device__ __forceinline__ int fv(int row) {
+    return kF32 ? 8 * ((row >> 2) & 1) : D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
+  }
 };
 
 template <typename T, int D>
 constexpr int paged_lds() {
-  return Team<T, D, 1>::kLdsTeam > 4 * Team<T, D, 4>::kLdsTeam ? Team<T, D, 1>::kLdsTeam
-                                                               : 4 * Team<T, D, 4>::kLdsTeam;
+  return Team<T, D, 1>::kLds > 4 * Team<T, D, 4>::kLds ? Team<T, D, 1>::kLds : 4 * Team<T, D, 4>::kLds;
 }
 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
+
+// 16 bytes a lane from global memory straight into LDS: lane i's go to lds + 16 i. lds is the same in all
+// lanes.
+__device__ __forceinline__ void load_lds(const char* base, unsigned off, char* lds) {
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base + off),
+                                   (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+
+// Waits until at most N of the wave's loads are on their way, and keeps reads of LDS behind that.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0f70);  // vmcnt(N)
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// The wave's reads of LDS have returned, and what it asks for next stays behind them.
+__device__ __forceinline__ void reads_done() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0)
+  __builtin_amdgcn_sched_barrier(0);
+}
 
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // to nearest, ties to even
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
@@ -120,13 +145,10 @@ template <typename T, int D, int KW>
 __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& job, char* lds) {
   using C = Team<T, D, KW>;
   constexpr bool F32 = C::kF32;
-  constexpr int NK = C::kKeys, NB = NK / 32, ND = D / 32, NP = C::kPieces;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5, col = lane & 31;
-  const int ttid = KW > 1 ? lane : tid;  // thread of the team
-  char* const my = KW > 1 ? lds + wave * C::kLdsTeam : lds;
-  char* const ldsk = my;
-  char* const ldsv = my + C::kLdsK;
-  int* const ldsp = (int*)(my + C::kLdsK + C::kLdsV);
+  constexpr int NK = C::kKeys, NB = NK / 32, ND = D / 32, NP = C::kPieces, RB = C::kRowBytes;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int half = lane >> 5, col = lane & 31;
+  char* const my = KW > 1 ? lds + wave * C::kLds : lds;
   const MapArgs& m = a.map;
   const int32_t* const table = m.table + (size_t)job.b * m.P;
   const int32_t* const pos = m.pos + (size_t)job.b * m.cap;
@@ -151,12 +173,13 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
   const bool idle = wrow0 >= job.rows;  // KW = 1: a wave without rows only loads
 
   // Q as the B operand: bf16: values 16 kk + 8 half ..; float32: values half D / 2 + 4 u ..
-  u32x4_t qf[F32 ? D / 8 : D / 16];
+  constexpr int NQ = F32 ? D / 8 : D / 16;
+  u32x4_t qf[NQ];
   {
-    const char* src = (const char*)a.q + qrow * C::kRowBytes;
+    const char* src = (const char*)a.q + qrow * RB;
 #pragma unroll
-    for (int i = 0; i < (F32 ? D / 8 : D / 16); ++i)
-      qf[i] = *(const u32x4_t*)(src + (F32 ? half * (D / 2) * 4 + 16 * i : 32 * i + 16 * half));
+    for (int i = 0; i < NQ; ++i)
+      qf[i] = *(const u32x4_t*)(src + (F32 ? half * (RB / 2) + 16 * i : 32 * i + 16 * half));
   }
 
   f32x16 O[ND];
@@ -166,222 +189,270 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     for (int i = 0; i < 16; ++i) O[d][i] = 0.f;
   float mx = -INFINITY, l = 0.f, sfx = 0.f;  // l and sfx: the lane's half of the keys
 
-  const int n_all = job.t_end;
+  const int t_end = job.t_end;
   const int t_first = KW > 1 ? job.t_begin + wave : job.t_begin;
-  const int end_slot = min(job.base + (min(job.row0 + (KW > 1 ? kWaveRows : kManyRows), job.rows) - 1) / a.G + 1,
-                           m.cap);  // slots from here on no row of the workgroup sees
-
-  u32x4_t kr[NP], vr[NP];
-  int pr = 0;
+  const int last_slot =  // the last one that any row of the workgroup sees
+      job.base + (min(job.row0 + (KW > 1 ? kWaveRows : kManyRows), job.rows) - 1) / a.G;
   auto slot_of = [&](int t) { return (t < job.sink_tiles ? t : t - job.sink_tiles + job.tile0) * NK; };
-  // Loads of a tile into registers: rows behind end_slot and rows of missing pages become zero.
-  auto load = [&](int t) {
-    const int s0 = slot_of(t);
-    const int r0 = ttid / (C::kRowBytes / 16), piece = ttid % (C::kRowBytes / 16);
+
+  // A tile comes in two steps: its columns of the table and its positions (a lane per slot, two tiles ahead),
+  // then its rows, straight into LDS (one tile ahead; no registers in between). A load instruction of a
+  // wave fills 1024 bytes of LDS in the order of its lanes, so the exchange of pieces is made on the
+  // global side: the lane at position p of a row loads piece p ^ f(row). Slots behind last_slot read as
+  // last_slot and slots of missing pages as page 0: no row sees them.
+  int tv, pv;  // table entry and position of the lane's slot
+  auto look = [&](int t) {
+    const int s = min(slot_of(t) + (lane & (NK - 1)), last_slot);
+    tv = table[s >> m.shift];
+    pv = pos[s];
+  };
+  const int lrow = lane / C::kRowPieces, piece = lane % C::kRowPieces;
+  const int load0 = KW > 1 ? 0 : wave * C::kWaveLoad;  // the wave's first row of a tile
+  struct Groups {
+    size_t at[C::kGroups];  // bytes of the group's first row in k and v
+    int most[C::kGroups];   // rows of the group from here on repeat it
+  };
+  auto groups = [&](int t) {
+    Groups gr;
+#pragma unroll
+    for (int i = 0; i < C::kGroups; ++i) {
+      const int r0 = (load0 & ~15) + 16 * i;
+      int page = __builtin_amdgcn_readlane(tv, r0);  // of slot min(s0 + r0, last_slot)
+      page = is_page(m, page) ? page : 0;
+      const int s = min(slot_of(t) + r0, last_slot & ~15);
+      gr.at[i] = ((((size_t)page * a.Hkv + job.h) << m.shift) + (s & ((1 << m.shift) - 1))) * RB;
+      gr.most[i] = last_slot - s;
+    }
+    return gr;
+  };
+  auto load_rows = [&](const Groups& gr, const void* pages, char* to, bool is_k) {
 #pragma unroll
     for (int u = 0; u < NP; ++u) {
-      const int s = s0 + r0 + u * C::kRowsStep;
-      const int page = s < end_slot ? table[s >> m.shift] : -1;
-      if (is_page(m, page)) {
-        const size_t at = ((((size_t)page * a.Hkv + job.h) << m.shift) + (s & ((1 << m.shift) - 1))) * C::kRowBytes + 16 * piece;
-        kr[u] = *(const u32x4_t*)((const char*)a.k + at);
-        vr[u] = *(const u32x4_t*)((const char*)a.v + at);
-      } else {
-        kr[u] = u32x4_t{};
-        vr[u] = u32x4_t{};
-      }
-    }
-    if (ttid < NK) {
-      const int s = s0 + ttid;
-      pr = s < end_slot && is_page(m, table[s >> m.shift]) ? pos[s] : kHidden;
+      const int i = u * C::kLoadRows / 16, row = (load0 + u * C::kLoadRows) | lrow;
+      const int r = min(row & 15, gr.most[i]);
+      const unsigned off = (unsigned)(r * RB + 16 * (piece ^ (is_k ? C::fk(row) : C::fv(row))));
+      load_lds((const char*)pages + gr.at[i], off, to + (load0 + u * C::kLoadRows) * RB);
     }
   };
-  auto store = [&]() {
-    const int r0 = ttid / (C::kRowBytes / 16), piece = ttid % (C::kRowBytes / 16);
-#pragma unroll
-    for (int u = 0; u < NP; ++u) {
-      const int r = r0 + u * C::kRowsStep;
-      *(u32x4_t*)(ldsk + r * C::kStrideK + 16 * piece) = kr[u];
-      *(u32x4_t*)(ldsv + r * C::kStrideV + 16 * piece) = vr[u];
-    }
-    if (ttid < NK) ldsp[ttid] = pr;
-  };
-  auto team_sync = [&]() {
-    if constexpr (KW > 1) {
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
-    } else {
+
+  // The lane's first addresses in a tile (see Team).
+  const int kx = col * RB + 16 * ((F32 ? half * (C::kRowPieces / 2) : half) ^ C::fk(col));
+  const int vx = F32 ? 4 * half * RB + 16 * ((col >> 2) ^ C::fv(4 * half)) + 4 * (col & 3)
+                     : (4 * half + ((lane & 15) >> 2)) * RB +
+                           16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ C::fv((lane & 15) >> 2)) +
+                           8 * (lane & 1);
+
+  int tp = 0;  // position of slot lane of the tile at hand, kHidden without a page
+  auto place = [&]() { return is_page(m, tv) ? pv : kHidden; };
+  // KW = 1: two buffers, one barrier a tile: a wave's rows have landed before it, so all have behind it,
+  // and the other buffer has been read. KW = 4: one buffer; K of the next tile is asked for when the scores are
+  // formed, V when the product is, and the waits count the loads that may be on their way behind those needed
+  // (loads land in order; others among them only make a wait longer).
+  char* cur = my;
+  if (t_first < t_end) {
+    look(t_first);
+    const Groups gr = groups(t_first);
+    tp = place();
+    load_rows(gr, a.k, cur, true);
+    if (t_first + KW < t_end) look(t_first + KW);
+    load_rows(gr, a.v, cur + C::kTile, false);
+  }
+  for (int t = t_first; t < t_end; t += KW) {
+    const bool more = t + KW < t_end;
+    int tp_next = 0;
+    Groups gr;
+    if constexpr (KW == 1) {
+      wait_loads<0>();
       __syncthreads();
-    }
-  };
-
-  if (t_first < n_all) load(t_first);
-  for (int t = t_first; t < n_all; t += KW) {
-    team_sync();  // the tile before is read
-    store();
-    team_sync();
-    if (t + KW < n_all) load(t + KW);
-    const int s0 = slot_of(t);
-    if (idle || s0 > slot_hi) continue;
-
-    // S^T, one 32 x 32 block per 32 keys
-    f32x16 S[NB];
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-#pragma unroll
-      for (int i = 0; i < 16; ++i) S[nb][i] = 0.f;
-      const char* row = ldsk + (32 * nb + col) * C::kStrideK;
-      if constexpr (F32) {
-#pragma unroll
-        for (int u = 0; u < D / 8; ++u) {
-          const u32x4_t kx = *(const u32x4_t*)(row + half * (D / 2) * 4 + 16 * u);
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            S[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(kx[e]), __uint_as_float(qf[u][e]),
-                                                         S[nb], 0, 0, 0);
-        }
-      } else {
-#pragma unroll
-        for (int kk = 0; kk < D / 16; ++kk)
-          S[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              __builtin_bit_cast(bf16x8, *(const u32x4_t*)(row + 32 * kk + 16 * half)),
-              __builtin_bit_cast(bf16x8, qf[kk]), S[nb], 0, 0, 0);
+      if (more) {
+        gr = groups(t + KW);
+        tp_next = place();
+        char* const other = cur == my ? my + 2 * C::kTile : my;
+        load_rows(gr, a.k, other, true);
+        load_rows(gr, a.v, other + C::kTile, false);
+        if (t + 2 * KW < t_end) look(t + 2 * KW);
       }
-    }
-
-    // What the tile needs compared, the same in all lanes.
-    const int tp = ldsp[lane & (NK - 1)];
-    const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
-    const bool hidden = __ballot(tp == kHidden) != 0;
-    const bool masked = hidden || s0 + NK - 1 > slot_lo ||
-                        (a.window > 0 && p_first <= win_hi && p_last >= a.n_sink);
-    // suffix: 0 none of the tile, 1 all of it, 2 compare
-    const int suf_how = a.suffix == nullptr && a.conf == nullptr ? 0
-                        : masked ? 2 : p_last <= suf_lo ? 0 : p_first > suf_hi ? 1 : 2;
-
-    float tmax = -INFINITY;
-    if (masked) {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = 32 * nb + 8 * (i >> 2) + 4 * half + (i & 3);
-          const int pj = ldsp[key];
-          const bool see = s0 + key <= slot_q && pj != kHidden && (pj > win || a.window == 0 || pj < a.n_sink);
-          S[nb][i] = see ? S[nb][i] * a.scale_log2 : -INFINITY;
-          tmax = fmaxf(tmax, S[nb][i]);
-        }
     } else {
+      wait_loads<NP>();  // K is here; V may be on its way
+    }
+    const int s0 = slot_of(t);
+    const char* const ldsk = cur;
+    const char* const ldsv = cur + C::kTile;
+    if (KW > 1 || (!idle && s0 <= slot_hi)) {
+      // S^T, one 32 x 32 block per 32 keys
+      f32x16 S[NB];
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
+      for (int nb = 0; nb < NB; ++nb) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          S[nb][i] *= a.scale_log2;
-          tmax = fmaxf(tmax, S[nb][i]);
+        for (int i = 0; i < 16; ++i) S[nb][i] = 0.f;
+#pragma unroll
+        for (int u = 0; u < NQ; ++u) {
+          const u32x4_t x = *(const u32x4_t*)(ldsk + (kx ^ (F32 ? 16 * u : 32 * u)) + 32 * nb * RB);
+          if constexpr (F32) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              S[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(qf[u][e]),
+                                                           S[nb], 0, 0, 0);
+          } else {
+            S[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
+                                                            __builtin_bit_cast(bf16x8, qf[u]), S[nb], 0, 0, 0);
+          }
         }
-    }
-    tmax = fmaxf(tmax, other_half(tmax));
-    const float m_new = fmaxf(mx, tmax);
-    const float ms = m_new == -INFINITY ? 0.f : m_new;  // a row that has seen nothing yet
-    if (__any(m_new > mx)) {
-      const float f = __builtin_amdgcn_exp2f(mx - ms);  // 0 from -inf
-      l *= f;
-      sfx *= f;
-#pragma unroll
-      for (int d = 0; d < ND; ++d)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) O[d][i] *= f;
-      mx = m_new;
-    }
-    float sum = 0.f;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        S[nb][i] = __builtin_amdgcn_exp2f(S[nb][i] - ms);
-        sum += S[nb][i];
       }
-    l += sum;
-    if (suf_how == 1) {
-      sfx += sum;
-    } else if (suf_how == 2) {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int key = 32 * nb + 8 * (i >> 2) + 4 * half + (i & 3);
-          sfx += ldsp[key] > suf ? S[nb][i] : 0.f;
-        }
-    }
 
-    bool odd = false;
-    if (masked) {
-      for (int i = lane; i < NK * (C::kRowBytes / 16); i += 64) {
-        const u32x4_t x = *(const u32x4_t*)(ldsv + i / (C::kRowBytes / 16) * C::kStrideV + i % (C::kRowBytes / 16) * 16);
-        odd |= odd_bits(x[0], F32) || odd_bits(x[1], F32) || odd_bits(x[2], F32) || odd_bits(x[3], F32);
-      }
-      odd = __any(odd);
-    }
-    if (!odd) {
-      // O^T += V^T P^T
-      if constexpr (F32) {
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const char* row = ldsv + (8 * (i >> 2) + 4 * half + (i & 3)) * C::kStrideV + 4 * col;
-#pragma unroll
-          for (int d = 0; d < ND; ++d)
-            O[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(*(const float*)(row + 128 * d), S[0][i], O[d], 0, 0, 0);
+      if constexpr (KW > 1) {
+        reads_done();
+        if (more) {
+          gr = groups(t + KW);
+          tp_next = place();
+          load_rows(gr, a.k, cur, true);
+          if (t + 2 * KW < t_end) look(t + 2 * KW);
         }
-      } else {
+      }
+
+      // What the tile needs compared, the same in all lanes.
+      const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
+      const bool masked = __ballot(tp == kHidden) != 0 || s0 + NK - 1 > slot_lo ||
+                          (a.window > 0 && p_first <= win_hi && p_last >= a.n_sink);
+      // suffix: 0 none of the tile, 1 all of it, 2 compare
+      const int suf_how = a.suffix == nullptr && a.conf == nullptr ? 0
+                          : masked ? 2 : p_last <= suf_lo ? 0 : p_first > suf_hi ? 1 : 2;
+      // position of accumulator row i of block nb, in the lane's half
+      auto pos_of = [&](int nb, int i) {
+        const int key = 32 * nb + 8 * (i >> 2) + (i & 3);
+        const int lo = __builtin_amdgcn_readlane(tp, key), hi = __builtin_amdgcn_readlane(tp, key + 4);
+        return half ? hi : lo;
+      };
+      auto sees = [&](int key, int pj) {
+        return s0 + key <= slot_q && pj != kHidden && (pj > win || a.window == 0 || pj < a.n_sink);
+      };
+      if (masked) {
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int s = 0; s < 2; ++s) {
-            u32x4_t p;  // the weights as bfloat16: the matrix product's type
-#pragma unroll
-            for (int e = 0; e < 4; ++e) p[e] = pack_bf16(S[nb][8 * s + 2 * e], S[nb][8 * s + 2 * e + 1]);
-            // a 16-lane group reads 4 keys x 16 values and gets them transposed: lane = value
-            const char* row = ldsv + (32 * nb + 16 * s + 4 * half + ((lane & 15) >> 2)) * C::kStrideV +
-                              32 * ((lane >> 4) & 1) + 8 * (lane & 3);
-#pragma unroll
-            for (int d = 0; d < ND; ++d) {
-              const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (__attribute__((address_space(3))) i16x4*)(row + 64 * d));
-              const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                  (__attribute__((address_space(3))) i16x4*)(row + 64 * d + 8 * C::kStrideV));
-              const u32x2_t x = __builtin_bit_cast(u32x2_t, lo), y = __builtin_bit_cast(u32x2_t, hi);
-              O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                  __builtin_bit_cast(bf16x8, u32x4_t{x[0], x[1], y[0], y[1]}), __builtin_bit_cast(bf16x8, p),
-                  O[d], 0, 0, 0);
-            }
-          }
+          for (int i = 0; i < 16; ++i)
+            S[nb][i] = sees(32 * nb + 8 * (i >> 2) + 4 * half + (i & 3), pos_of(nb, i)) ? S[nb][i] : -INFINITY;
       }
-    } else {
-      // A value that is not finite in a tile that not every row sees: term by term, seen slots only.
+      float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
+        for (int i = 0; i < 16; ++i) t4[i & 3] = fmaxf(t4[i & 3], S[nb][i]);
+      float tmax = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+      tmax = fmaxf(tmax, other_half(tmax)) * a.scale_log2;
+      // The running maximum follows only when a score passes it by kSlack: weights are then at most
+      // 2^kSlack, which costs no precision, and most tiles leave O as it is. A row goes by its own scores
+      // alone.
+      const bool raise = tmax > mx + kSlack;
+      if (__any(raise)) {
+        const float m_new = raise ? tmax : mx;
+        const float f = raise ? __builtin_amdgcn_exp2f(mx - tmax) : 1.f;  // 0 where nothing was seen before
+        l *= f;
+        sfx *= f;
 #pragma unroll
-          for (int hh = 0; hh < 2; ++hh) {
-            const int key = 32 * nb + 8 * (i >> 2) + 4 * hh + (i & 3);
-            const float p = __shfl(S[nb][i], 32 * hh + col, 64);
-            const int pj = ldsp[key];
-            const bool see = s0 + key <= slot_q && pj != kHidden && (pj > win || a.window == 0 || pj < a.n_sink);
-            if (see) {
+        for (int d = 0; d < ND; ++d)
 #pragma unroll
-              for (int d = 0; d < ND; ++d)
+          for (int i = 0; i < 16; ++i) O[d][i] *= f;
+        mx = m_new;
+      }
+      const float ms = mx == -INFINITY ? 0.f : mx;
+      float s4[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                  const int dd = 32 * d + 8 * (e >> 2) + 4 * half + (e & 3);
-                  const float x = F32 ? *(const float*)(ldsv + key * C::kStrideV + 4 * dd)
-                                      : __uint_as_float((uint32_t)*(const uint16_t*)(ldsv + key * C::kStrideV + 2 * dd) << 16);
-                  O[d][e] += p * x;
-                }
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          S[nb][i] = __builtin_amdgcn_exp2f(fmaf(S[nb][i], a.scale_log2, -ms));
+          s4[i & 3] += S[nb][i];
+        }
+      const float sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
+      l += sum;
+      if (suf_how == 1) {
+        sfx += sum;
+      } else if (suf_how == 2) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sfx += pos_of(nb, i) > suf ? S[nb][i] : 0.f;
+      }
+
+      if constexpr (KW > 1) {
+        if (more)
+          wait_loads<NP>();  // V is here; K of the next tile may be on its way
+        else
+          wait_loads<0>();
+      }
+      bool odd = false;
+      if (masked) {
+#pragma unroll 4
+        for (int i = lane; i < C::kTile / 16; i += 64) {
+          const u32x4_t x = *(const u32x4_t*)(ldsv + 16 * i);
+          odd |= odd_bits(x[0], F32) || odd_bits(x[1], F32) || odd_bits(x[2], F32) || odd_bits(x[3], F32);
+        }
+        odd = __any(odd);
+      }
+      if (!odd) {
+        // O^T += V^T P^T
+        if constexpr (F32) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+              O[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(
+                  *(const float*)(ldsv + (vx ^ (128 * d)) + (8 * (i >> 2) + (i & 3)) * RB), S[0][i], O[d], 0, 0, 0);
+        } else {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              u32x4_t p;  // the weights as bfloat16: the matrix product's type
+#pragma unroll
+              for (int e = 0; e < 4; ++e) p[e] = pack_bf16(S[nb][8 * s + 2 * e], S[nb][8 * s + 2 * e + 1]);
+              // a 16-lane group reads 4 keys x 16 values and gets them transposed: lane = value
+#pragma unroll
+              for (int d = 0; d < ND; ++d) {
+                const char* at = ldsv + (vx ^ (64 * d)) + (32 * nb + 16 * s) * RB;
+                const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) i16x4*)at);
+                const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                    (__attribute__((address_space(3))) i16x4*)(at + 8 * RB));
+                const u32x2_t x = __builtin_bit_cast(u32x2_t, lo), y = __builtin_bit_cast(u32x2_t, hi);
+                O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                    __builtin_bit_cast(bf16x8, u32x4_t{x[0], x[1], y[0], y[1]}), __builtin_bit_cast(bf16x8, p),
+                    O[d], 0, 0, 0);
+              }
             }
-          }
+        }
+      } else {
+        // A value that is not finite in a tile that not every row sees: term by term, seen slots only.
+#pragma unroll 1
+        for (int key = 0; key < NK; ++key) {
+          const int at = (key >> 5) * 16 + ((key >> 3) & 3) * 4 + (key & 3);
+          float p = 0.f;
+#pragma unroll
+          for (int i = 0; i < 16 * NB; ++i) p = at == i ? S[i >> 4][i & 15] : p;
+          p = __shfl(p, 32 * ((key >> 2) & 1) + col, 64);
+          const bool see = sees(key, __builtin_amdgcn_readlane(tp, key));
+          const char* row = ldsv + key * RB;
+          const int fv = C::fv(key);
+#pragma unroll
+          for (int d = 0; d < ND; ++d)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const int byte = (32 * d + 8 * (e >> 2) + 4 * half + (e & 3)) * (int)sizeof(T);
+              const char* src = row + (((byte >> 4) ^ fv) << 4) + (byte & 15);
+              const float x = F32 ? *(const float*)src : __uint_as_float((uint32_t)*(const uint16_t*)src << 16);
+              O[d][e] = see ? fmaf(p, x, O[d][e]) : O[d][e];
+            }
+        }
+      }
     }
+    if constexpr (KW > 1) {
+      reads_done();
+      if (more) load_rows(gr, a.v, cur + C::kTile, false);
+    } else {
+      cur = cur == my ? my + 2 * C::kTile : my;
+    }
+    tp = tp_next;
   }
 
   l += other_half(l);
@@ -426,7 +497,6 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     // Join the four waves: their numerators and statistics through LDS, 8 threads a row.
     float* const num = (float*)my;
     float* const st = num + kWaveRows * (D + 4);
-    team_sync();
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -445,14 +515,14 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     float wm[4], M = -INFINITY;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      wm[w] = ((const float*)(lds + w * C::kLdsTeam))[kStatAt + r];
+      wm[w] = ((const float*)(lds + w * C::kLds))[kStatAt + r];
       M = fmaxf(M, wm[w]);
     }
     const float Ms = M == -INFINITY ? 0.f : M;
     float L = 0.f, SF = 0.f, x[D / 8] = {};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float* src = (const float*)(lds + w * C::kLdsTeam);
+      const float* src = (const float*)(lds + w * C::kLds);
       const float f = __builtin_amdgcn_exp2f(wm[w] - Ms);
       L += f * src[kStatAt + kWaveRows + r];
       SF += f * src[kStatAt + 2 * kWaveRows + r];
@@ -521,7 +591,7 @@ __device__ __forceinline__ void job_tiles(const PagedAttendArgs& a, Job& job, in
 // sequence are Hkv apart, so with 8 heads (the XCDs are dealt workgroups in turn) they share an L2. The
 // tiles of many rows come first, the last of a sequence (the longest) before the others.
 template <typename T, int D>
-__global__ __launch_bounds__(kPagedThreads) void paged_attend(PagedAttendArgs a) {
+__global__ __launch_bounds__(kPagedThreads, 2) void paged_attend(PagedAttendArgs a) {
   __shared__ __align__(16) char lds[paged_lds<T, D>()];
   const int per = a.Hkv * a.ns;
   const int unit = blockIdx.x / per, rest = blockIdx.x % per;
