@@ -24,6 +24,8 @@
 // number and position. There a value that some row does not see could still reach it as 0 x inf = NaN
 // through the matrix product: when such a tile holds a value that is not finite, its product is
 // formed term by term for the rows that see it.
+#include <type_traits>
+
 #include "lg_paged_internal.h"
 
 namespace lg {
@@ -61,7 +63,7 @@ struct PagedAttendArgs {
 // A row of K or V in LDS is its 16-byte pieces in the order piece ^ f(row): the 16 rows whose pieces one read
 // of K takes, and the 4 rows (of 64 bytes) that a transposed read of V takes, then lie in different banks,
 // without padding. The rows a lane reads differ from its first one by multiples that leave f as it is, so the
-// exchange is one xor with a constant on its first address.
+// exchange is one xor with a constant on its first address (tiles lie at multiples of 1024 bytes).
 template <typename T, int D, int KW>
 struct Team {
   static constexpr bool kF32 = sizeof(T) == 4;
@@ -84,18 +86,31 @@ struct Team {
   }
 };
 
+// Tiles whose table entries and positions (64 of each) a wave holds at once.
+constexpr int kRing = 3 * 512;
+
 template <typename T, int D>
 constexpr int paged_lds() {
-  return Team<T, D, 1>::kLds > 4 * Team<T, D, 4>::kLds ? Team<T, D, 1>::kLds : 4 * Team<T, D, 4>::kLds;
+  constexpr int many = Team<T, D, 1>::kLds + 4 * kRing, few = 4 * (Team<T, D, 4>::kLds + kRing);
+  return (many > few ? many : few) + 16;
 }
 
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32, 64); }
+// The value of lane ^ 32.
+__device__ __forceinline__ float other_half(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 32) != 0 ? r[0] : r[1]);
+}
 
 // 16 bytes a lane from global memory straight into LDS: lane i's go to lds + 16 i. lds is the same in all
 // lanes.
 __device__ __forceinline__ void load_lds(const char* base, unsigned off, char* lds) {
   __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(base + off),
                                    (__attribute__((address_space(3))) void*)lds, 16, 0, 0);
+}
+
+__device__ __forceinline__ void load_lds4(const int32_t* from, int32_t* lds) {  // 4 bytes a lane, likewise
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)lds, 4, 0, 0);
 }
 
 // Waits until at most N of the wave's loads are on their way, and keeps reads of LDS behind that.
@@ -128,6 +143,18 @@ __device__ __forceinline__ void raise_conf(float* conf, float mass) {
   atomicMax((int*)conf, mass != mass ? 0x7fc00000 : __float_as_int(mass));
 }
 
+// Order for the scheduler: the scores of 64 keys' 16 reads of LDS and 16 matrix instructions, the reads 8
+// ahead (left to itself it reads 2 ahead; 462 us for a chunk of 4096 tokens behind 4096, 455 with this).
+__device__ __forceinline__ void schedule_scores() {
+  __builtin_amdgcn_sched_group_barrier(0x100, 8, 0);  // reads of LDS
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix instructions
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
+}
+
 // What a workgroup attends with: its rows, and the slots that any of them may see.
 struct Job {
   int b, h;         // sequence, KV head
@@ -148,7 +175,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
   constexpr int NK = C::kKeys, NB = NK / 32, ND = D / 32, NP = C::kPieces, RB = C::kRowBytes;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, col = lane & 31;
-  char* const my = KW > 1 ? lds + wave * C::kLds : lds;
+  char* const my = KW > 1 ? lds + wave * (C::kLds + kRing) : lds;
   const MapArgs& m = a.map;
   const int32_t* const table = m.table + (size_t)job.b * m.P;
   const int32_t* const pos = m.pos + (size_t)job.b * m.cap;
@@ -193,26 +220,30 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
   const int t_first = KW > 1 ? job.t_begin + wave : job.t_begin;
   const int last_slot =  // the last one that any row of the workgroup sees
       job.base + (min(job.row0 + (KW > 1 ? kWaveRows : kManyRows), job.rows) - 1) / a.G;
-  auto slot_of = [&](int t) { return (t < job.sink_tiles ? t : t - job.sink_tiles + job.tile0) * NK; };
+  auto slot_of = [&](int t) __attribute__((always_inline)) { return (t < job.sink_tiles ? t : t - job.sink_tiles + job.tile0) * NK; };
 
-  // A tile comes in two steps: its columns of the table and its positions (a lane per slot, two tiles ahead),
-  // then its rows, straight into LDS (one tile ahead; no registers in between). A load instruction of a
-  // wave fills 1024 bytes of LDS in the order of its lanes, so the exchange of pieces is made on the
-  // global side: the lane at position p of a row loads piece p ^ f(row). Slots behind last_slot read as
-  // last_slot and slots of missing pages as page 0: no row sees them.
-  int tv, pv;  // table entry and position of the lane's slot
-  auto look = [&](int t) {
-    const int s = min(slot_of(t) + (lane & (NK - 1)), last_slot);
-    tv = table[s >> m.shift];
-    pv = pos[s];
+  // A tile comes in two steps: its columns of the table and its positions (a lane per slot), then its rows,
+  // both straight into LDS, with no registers in between. A load instruction of a wave fills LDS in the
+  // order of its lanes, so the exchange of a row's pieces is made on the global side: the lane at position
+  // p of a row loads piece p ^ f(row). Slots behind last_slot read as last_slot and slots of missing pages
+  // as page 0: no row sees them.
+  int32_t* const ring = (int32_t*)(my + C::kLds + (KW > 1 ? 0 : wave * kRing));
+  int32_t* const odd = (int32_t*)(lds + paged_lds<T, D>() - 16) + (KW > 1 ? wave : 0);  // see make_finite
+  auto look = [&](int t, int32_t* __restrict__ to) __attribute__((always_inline)) {
+    const int s = min(slot_of(min(t, t_end - 1)) + (lane & (NK - 1)), last_slot);
+    load_lds4(table + (s >> m.shift), to);
+    load_lds4(pos + s, to + 64);
   };
+  // The position of the lane's slot, kHidden without a page.
+  auto place = [&](const int32_t* at) __attribute__((always_inline)) { return is_page(m, at[lane]) ? at[64 + lane] : kHidden; };
   const int lrow = lane / C::kRowPieces, piece = lane % C::kRowPieces;
   const int load0 = KW > 1 ? 0 : wave * C::kWaveLoad;  // the wave's first row of a tile
   struct Groups {
     size_t at[C::kGroups];  // bytes of the group's first row in k and v
     int most[C::kGroups];   // rows of the group from here on repeat it
   };
-  auto groups = [&](int t) {
+  auto groups = [&](int t, const int32_t* at) __attribute__((always_inline)) {
+    const int tv = at[lane];
     Groups gr;
 #pragma unroll
     for (int i = 0; i < C::kGroups; ++i) {
@@ -225,13 +256,22 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     }
     return gr;
   };
-  auto load_rows = [&](const Groups& gr, const void* pages, char* to, bool is_k) {
+  // Rows of a tile to LDS at `to` + off. A group with all its rows (all but the last of a sequence) needs
+  // one offset a lane; the rest is in the instruction and an exclusive or.
+  const int lk = lrow * RB + 16 * (piece ^ C::fk(load0 | lrow)), lv = lrow * RB + 16 * (piece ^ C::fv(load0 | lrow));
+  auto load_rows = [&](const Groups& gr, const void* pages, char* to, int off, bool is_k) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < NP; ++u) {
-      const int i = u * C::kLoadRows / 16, row = (load0 + u * C::kLoadRows) | lrow;
-      const int r = min(row & 15, gr.most[i]);
-      const unsigned off = (unsigned)(r * RB + 16 * (piece ^ (is_k ? C::fk(row) : C::fv(row))));
-      load_lds((const char*)pages + gr.at[i], off, to + (load0 + u * C::kLoadRows) * RB);
+    for (int i = 0; i < C::kGroups; ++i) {
+      const char* base = (const char*)pages + gr.at[i];
+      const bool whole = gr.most[i] >= 15;
+#pragma unroll
+      for (int u = i * NP / C::kGroups; u < (i + 1) * NP / C::kGroups; ++u) {
+        const int up = u * C::kLoadRows, row = (load0 + up) | lrow;
+        unsigned at = (is_k ? lk ^ (16 * C::fk(up)) : lv ^ (16 * C::fv(up))) + ((load0 + up) & 15) * RB;
+        if (!whole)
+          at = (unsigned)(min(row & 15, gr.most[i]) * RB + 16 * (piece ^ (is_k ? C::fk(row) : C::fv(row))));
+        load_lds(base, at, to + off + (load0 + up) * RB);
+      }
     }
   };
 
@@ -242,217 +282,272 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
                            16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ C::fv((lane & 15) >> 2)) +
                            8 * (lane & 1);
 
-  int tp = 0;  // position of slot lane of the tile at hand, kHidden without a page
-  auto place = [&]() { return is_page(m, tv) ? pv : kHidden; };
-  // KW = 1: two buffers, one barrier a tile: a wave's rows have landed before it, so all have behind it,
-  // and the other buffer has been read. KW = 4: one buffer; K of the next tile is asked for when the scores are
-  // formed, V when the product is, and the waits count the loads that may be on their way behind those needed
-  // (loads land in order; others among them only make a wait longer).
-  char* cur = my;
-  if (t_first < t_end) {
-    look(t_first);
-    const Groups gr = groups(t_first);
-    tp = place();
-    load_rows(gr, a.k, cur, true);
-    if (t_first + KW < t_end) look(t_first + KW);
-    load_rows(gr, a.v, cur + C::kTile, false);
-  }
-  for (int t = t_first; t < t_end; t += KW) {
-    const bool more = t + KW < t_end;
-    int tp_next = 0;
-    Groups gr;
-    if constexpr (KW == 1) {
-      wait_loads<0>();
-      __syncthreads();
-      if (more) {
-        gr = groups(t + KW);
-        tp_next = place();
-        char* const other = cur == my ? my + 2 * C::kTile : my;
-        load_rows(gr, a.k, other, true);
-        load_rows(gr, a.v, other + C::kTile, false);
-        if (t + 2 * KW < t_end) look(t + 2 * KW);
+  // S^T of 32 keys of a tile
+  auto scores = [&](const char* from, int k, f32x16& S) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll
+    for (int u = 0; u < NQ; ++u) {
+      const u32x4_t x = *(const u32x4_t*)(from + ((k + kx) ^ (F32 ? 16 * u : 32 * u)));
+      if constexpr (F32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          S = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(qf[u][e]), S, 0, 0, 0);
+      } else {
+        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, qf[u]),
+                                                    S, 0, 0, 0);
       }
-    } else {
-      wait_loads<NP>();  // K is here; V may be on its way
     }
-    const int s0 = slot_of(t);
-    const char* const ldsk = cur;
-    const char* const ldsv = cur + C::kTile;
-    if (KW > 1 || (!idle && s0 <= slot_hi)) {
-      // S^T, one 32 x 32 block per 32 keys
-      f32x16 S[NB];
+  };
+  // Maximum of the lane's row over the block, both halves
+  auto top = [&](const f32x16& S) __attribute__((always_inline)) {
+    float t4[4] = {S[0], S[1], S[2], S[3]};
 #pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
+    for (int i = 4; i < 16; ++i) t4[i & 3] = fmaxf(t4[i & 3], S[i]);
+    const float x = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+    return fmaxf(x, other_half(x));
+  };
+
+  // What a tile needs compared, the same in all lanes; tp: its positions, a lane per slot.
+  int s0, tp;
+  bool masked;
+  // position of accumulator row i of block nb, in the lane's half
+  auto pos_of = [&](int nb, int i) __attribute__((always_inline)) {
+    const int key = 32 * nb + 8 * (i >> 2) + (i & 3);
+    const int lo = __builtin_amdgcn_readlane(tp, key), hi = __builtin_amdgcn_readlane(tp, key + 4);
+    return half ? hi : lo;
+  };
+  auto sees = [&](int key, int pj) __attribute__((always_inline)) {
+    return s0 + key <= slot_q && pj != kHidden && (pj > win || a.window == 0 || pj < a.n_sink);
+  };
+  auto is_masked = [&]() __attribute__((always_inline)) {
+    const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
+    return __ballot(tp == kHidden) != 0 || s0 + NK - 1 > slot_lo ||
+           (a.window > 0 && p_first <= win_hi && p_last >= a.n_sink);
+  };
+  auto mask = [&](f32x16& S, int nb) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) S[nb][i] = 0.f;
+    for (int i = 0; i < 16; ++i)
+      S[i] = sees(32 * nb + 8 * (i >> 2) + 4 * half + (i & 3), pos_of(nb, i)) ? S[i] : -INFINITY;
+  };
+  // The running maximum follows only when a score passes it by kSlack: weights are then at most 2^kSlack,
+  // which costs no precision, and most tiles leave O as it is. A row goes by its own scores alone.
+  auto raise_max = [&](float most) __attribute__((always_inline)) {
+    const float tmax = most * a.scale_log2;
+    const bool raise = tmax > mx + kSlack;
+    if (__any(raise)) {
+      const float f = raise ? __builtin_amdgcn_exp2f(mx - tmax) : 1.f;  // 0 where nothing was seen before
+      mx = raise ? tmax : mx;
+      l *= f;
+      sfx *= f;
 #pragma unroll
-        for (int u = 0; u < NQ; ++u) {
-          const u32x4_t x = *(const u32x4_t*)(ldsk + (kx ^ (F32 ? 16 * u : 32 * u)) + 32 * nb * RB);
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[d][i] *= f;
+    }
+  };
+  // The suffix's share of a tile: none, all, or slot by slot
+  enum { kNone, kAll, kSome };
+  auto suffix_of = [&]() __attribute__((always_inline)) {
+    if (a.suffix == nullptr && a.conf == nullptr) return (int)kNone;
+    const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
+    return masked ? (int)kSome : p_last <= suf_lo ? (int)kNone : p_first > suf_hi ? (int)kAll : (int)kSome;
+  };
+  auto weight = [&](float s) __attribute__((always_inline)) {
+    return __builtin_amdgcn_exp2f(fmaf(s, a.scale_log2, mx == -INFINITY ? 0.f : -mx));
+  };
+  auto add_suffix = [&](const f32x16& S, int nb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) sfx += pos_of(nb, i) > suf ? weight(S[i]) : 0.f;
+  };
+  // S becomes the weights; returns their sum over the lane's half.
+  auto weights = [&](f32x16& S) __attribute__((always_inline)) {
+    float s4[4];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      S[i] = weight(S[i]);
+      s4[i & 3] = i < 4 ? S[i] : s4[i & 3] + S[i];
+    }
+    return (s4[0] + s4[1]) + (s4[2] + s4[3]);
+  };
+  // Puts 0 in the place of what is not finite in V of a tile (in LDS), and says so in *odd. With KW = 1 other waves
+  // may read the tile meanwhile: they find a value or its 0, and the pass behind the loop adds the value.
+  auto make_finite = [&](char* v) __attribute__((always_inline)) {
+    for (int i = lane; i < C::kTile / 16; i += 64) {
+      u32x4_t x = *(const u32x4_t*)(v + 16 * i);
+      if (odd_bits(x[0], F32) || odd_bits(x[1], F32) || odd_bits(x[2], F32) || odd_bits(x[3], F32)) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
           if constexpr (F32) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              S[nb] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(qf[u][e]),
-                                                           S[nb], 0, 0, 0);
+            if (odd_bits(x[e], true)) x[e] = 0;
           } else {
-            S[nb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
-                                                            __builtin_bit_cast(bf16x8, qf[u]), S[nb], 0, 0, 0);
+            if ((x[e] & 0x7f80u) == 0x7f80u) x[e] &= 0xffff0000u;
+            if ((x[e] & 0x7f800000u) == 0x7f800000u) x[e] &= 0xffffu;
           }
         }
+        *(u32x4_t*)(v + 16 * i) = x;
+        *odd = 1;
       }
+    }
+  };
 
-      if constexpr (KW > 1) {
-        reads_done();
-        if (more) {
-          gr = groups(t + KW);
-          tp_next = place();
-          load_rows(gr, a.k, cur, true);
-          if (t + 2 * KW < t_end) look(t + 2 * KW);
+  // O^T += V^T P^T over 32 keys
+  auto product = [&](const char* from, int v, const f32x16& P) __attribute__((always_inline)) {
+    if constexpr (F32) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const float x = *(const float*)(from + ((v + vx) ^ (128 * d)) + (8 * (i >> 2) + (i & 3)) * RB);
+          O[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, P[i], O[d], 0, 0, 0);
+        }
+    } else {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        u32x4_t p;  // the weights as bfloat16: the matrix product's type
+#pragma unroll
+        for (int e = 0; e < 4; ++e) p[e] = pack_bf16(P[8 * s + 2 * e], P[8 * s + 2 * e + 1]);
+        // a 16-lane group reads 4 keys x 16 values and gets them transposed: lane = value
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const char* at = from + ((v + vx) ^ (64 * d)) + 16 * s * RB;
+          const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at);
+          const i16x4 hi =
+              __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(at + 8 * RB));
+          const u32x2_t x = __builtin_bit_cast(u32x2_t, lo), y = __builtin_bit_cast(u32x2_t, hi);
+          const u32x4_t z = {x[0], x[1], y[0], y[1]};
+          O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, z), __builtin_bit_cast(bf16x8, p),
+                                                         O[d], 0, 0, 0);
         }
       }
+    }
+  };
+  constexpr int kBlock = 32 * RB;  // bytes of 32 keys
 
-      // What the tile needs compared, the same in all lanes.
-      const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
-      const bool masked = __ballot(tp == kHidden) != 0 || s0 + NK - 1 > slot_lo ||
-                          (a.window > 0 && p_first <= win_hi && p_last >= a.n_sink);
-      // suffix: 0 none of the tile, 1 all of it, 2 compare
-      const int suf_how = a.suffix == nullptr && a.conf == nullptr ? 0
-                          : masked ? 2 : p_last <= suf_lo ? 0 : p_first > suf_hi ? 1 : 2;
-      // position of accumulator row i of block nb, in the lane's half
-      auto pos_of = [&](int nb, int i) {
-        const int key = 32 * nb + 8 * (i >> 2) + (i & 3);
-        const int lo = __builtin_amdgcn_readlane(tp, key), hi = __builtin_amdgcn_readlane(tp, key + 4);
-        return half ? hi : lo;
-      };
-      auto sees = [&](int key, int pj) {
-        return s0 + key <= slot_q && pj != kHidden && (pj > win || a.window == 0 || pj < a.n_sink);
-      };
-      if (masked) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            S[nb][i] = sees(32 * nb + 8 * (i >> 2) + 4 * half + (i & 3), pos_of(nb, i)) ? S[nb][i] : -INFINITY;
+  // KW = 1: two buffers and one barrier a tile: a wave's loads have landed before it, so all have behind it, and
+  // what the loads behind it fill has been read. KW = 4: one buffer; K of the next tile is asked for when the
+  // scores are formed, V when the product is, and the waits count the loads that may be on their way behind
+  // those needed (loads land in order; others among them only make a wait longer). The tile functions take
+  // what they fill and what they read as pointers that do not alias: the compiler would make every read wait for
+  // every load.
+  const int step = KW;
+  if (KW > 1 || tid == 0) *odd = 0;
+  if constexpr (KW == 1) __syncthreads();
+  if (t_first < t_end) {
+    look(t_first, ring);
+    wait_loads<0>();
+    const Groups gr = groups(t_first, ring);
+    load_rows(gr, a.k, my, 0, true);
+    look(t_first + step, ring + 128);
+    load_rows(gr, a.v, my, C::kTile, false);
+  }
+  if constexpr (KW == 1) {
+    auto tile = [&](int t, int at, const char* __restrict__ from, char* __restrict__ to, const Groups& gr,
+                    int32_t* __restrict__ ring_to) __attribute__((always_inline)) {
+      const int other = 2 * C::kTile - at;
+      if (t + 1 < t_end) {
+        load_rows(gr, a.k, to, other, true);
+        load_rows(gr, a.v, to, other + C::kTile, false);
       }
-      float t4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) t4[i & 3] = fmaxf(t4[i & 3], S[nb][i]);
-      float tmax = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
-      tmax = fmaxf(tmax, other_half(tmax)) * a.scale_log2;
-      // The running maximum follows only when a score passes it by kSlack: weights are then at most
-      // 2^kSlack, which costs no precision, and most tiles leave O as it is. A row goes by its own scores
-      // alone.
-      const bool raise = tmax > mx + kSlack;
-      if (__any(raise)) {
-        const float m_new = raise ? tmax : mx;
-        const float f = raise ? __builtin_amdgcn_exp2f(mx - tmax) : 1.f;  // 0 where nothing was seen before
-        l *= f;
-        sfx *= f;
+      look(t + 2, ring_to);
+      if (idle || s0 > slot_hi) return;
+      f32x16 S, S1;
+      scores(from, at, S);
+      if constexpr (NB > 1) {
+        scores(from, at + kBlock, S1);
+        schedule_scores();
+      }
+      masked = is_masked();
+      const int how = suffix_of();
+      if (masked) {
+        make_finite(const_cast<char*>(from) + at + C::kTile);
+        mask(S, 0);
+        if constexpr (NB > 1) mask(S1, 1);
+      }
+      raise_max(NB > 1 ? fmaxf(top(S), top(S1)) : top(S));
+      if (how == kSome) {
+        add_suffix(S, 0);
+        if constexpr (NB > 1) add_suffix(S1, 1);
+      }
+      // From here on without a branch: the second block's exponentials beside the first one's product.
+      float sum = weights(S);
+      product(from, at + C::kTile, S);
+      if constexpr (NB > 1) {
+        sum += weights(S1);
+        product(from, at + C::kTile + kBlock, S1);
+      }
+      l += sum;
+      sfx += how == kAll ? sum : 0.f;
+    };
+    for (int t = t_first, n = 0; t < t_end; ++t, n = n == 2 ? 0 : n + 1) {
+      wait_loads<0>();
+      __syncthreads();
+      const int n1 = n == 2 ? 0 : n + 1, n2 = n1 == 2 ? 0 : n1 + 1;
+      const Groups gr = groups(t + 1, ring + 128 * n1);
+      tp = place(ring + 128 * n);
+      s0 = slot_of(t);
+      tile(t, (t - t_first & 1) * 2 * C::kTile, my, my, gr, ring + 128 * n2);
+    }
+  } else {
+    auto behind_scores = [&](int t, bool more, const Groups& gr, f32x16& S, const char* __restrict__ from,
+                             char* __restrict__ to, int32_t* __restrict__ ring_to) __attribute__((always_inline)) {
+      if (more) load_rows(gr, a.k, to, 0, true);
+      look(t + 2 * KW, ring_to);
+      masked = is_masked();
+      const int how = suffix_of();
+      if (masked) mask(S, 0);
+      raise_max(top(S));
+      if (how == kSome) add_suffix(S, 0);
+      const float sum = weights(S);
+      l += sum;
+      sfx += how == kAll ? sum : 0.f;
+      if (more)
+        wait_loads<NP>();  // V is here; K of the next tile may be on its way
+      else
+        wait_loads<0>();
+      if (masked) make_finite(const_cast<char*>(from) + C::kTile);
+      product(from, C::kTile, S);
+    };
+    for (int t = t_first, n = 0; t < t_end; t += KW, n = n == 2 ? 0 : n + 1) {
+      const bool more = t + KW < t_end;
+      wait_loads<NP>();  // K is here; V may be on its way
+      const int n1 = n == 2 ? 0 : n + 1, n2 = n1 == 2 ? 0 : n1 + 1;
+      const Groups gr = groups(t + KW, ring + 128 * n1);
+      tp = place(ring + 128 * n);
+      s0 = slot_of(t);
+      f32x16 S;
+      scores(my, 0, S);
+      reads_done();
+      behind_scores(t, more, gr, S, my, my, ring + 128 * n2);
+      reads_done();
+      if (more) load_rows(gr, a.v, my, C::kTile, false);
+    }
+    wait_loads<0>();
+  }
+
+  // Values that are not finite in tiles that not every row sees counted as 0 so far. To a row that sees one with a
+  // weight above 0 it is what it is, whatever that weight: added here, slot by slot (again where a
+  // product has it already, which changes nothing).
+  if constexpr (KW == 1) __syncthreads();
+  if (*odd != 0) {
+    for (int t = t_first; t < t_end; t += KW) {
+      s0 = slot_of(t);
+      if (idle || s0 > slot_hi) continue;
+      for (int key = 0; key < NK; ++key) {
+        const int j = min(s0 + key, last_slot);
+        const int page = table[j >> m.shift];
+        if (!is_page(m, page) || !sees(key, pos[j])) continue;
+        const T* row = (const T*)a.v +
+                       ((((size_t)page * a.Hkv + job.h) << m.shift) + (j & ((1 << m.shift) - 1))) * D + 4 * half;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
-          for (int i = 0; i < 16; ++i) O[d][i] *= f;
-        mx = m_new;
-      }
-      const float ms = mx == -INFINITY ? 0.f : mx;
-      float s4[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          S[nb][i] = __builtin_amdgcn_exp2f(fmaf(S[nb][i], a.scale_log2, -ms));
-          s4[i & 3] += S[nb][i];
-        }
-      const float sum = (s4[0] + s4[1]) + (s4[2] + s4[3]);
-      l += sum;
-      if (suf_how == 1) {
-        sfx += sum;
-      } else if (suf_how == 2) {
-#pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) sfx += pos_of(nb, i) > suf ? S[nb][i] : 0.f;
-      }
-
-      if constexpr (KW > 1) {
-        if (more)
-          wait_loads<NP>();  // V is here; K of the next tile may be on its way
-        else
-          wait_loads<0>();
-      }
-      bool odd = false;
-      if (masked) {
-#pragma unroll 4
-        for (int i = lane; i < C::kTile / 16; i += 64) {
-          const u32x4_t x = *(const u32x4_t*)(ldsv + 16 * i);
-          odd |= odd_bits(x[0], F32) || odd_bits(x[1], F32) || odd_bits(x[2], F32) || odd_bits(x[3], F32);
-        }
-        odd = __any(odd);
-      }
-      if (!odd) {
-        // O^T += V^T P^T
-        if constexpr (F32) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-#pragma unroll
-            for (int d = 0; d < ND; ++d)
-              O[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(
-                  *(const float*)(ldsv + (vx ^ (128 * d)) + (8 * (i >> 2) + (i & 3)) * RB), S[0][i], O[d], 0, 0, 0);
-        } else {
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-              u32x4_t p;  // the weights as bfloat16: the matrix product's type
-#pragma unroll
-              for (int e = 0; e < 4; ++e) p[e] = pack_bf16(S[nb][8 * s + 2 * e], S[nb][8 * s + 2 * e + 1]);
-              // a 16-lane group reads 4 keys x 16 values and gets them transposed: lane = value
-#pragma unroll
-              for (int d = 0; d < ND; ++d) {
-                const char* at = ldsv + (vx ^ (64 * d)) + (32 * nb + 16 * s) * RB;
-                const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) i16x4*)at);
-                const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                    (__attribute__((address_space(3))) i16x4*)(at + 8 * RB));
-                const u32x2_t x = __builtin_bit_cast(u32x2_t, lo), y = __builtin_bit_cast(u32x2_t, hi);
-                O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    __builtin_bit_cast(bf16x8, u32x4_t{x[0], x[1], y[0], y[1]}), __builtin_bit_cast(bf16x8, p),
-                    O[d], 0, 0, 0);
-              }
-            }
-        }
-      } else {
-        // A value that is not finite in a tile that not every row sees: term by term, seen slots only.
-#pragma unroll 1
-        for (int key = 0; key < NK; ++key) {
-          const int at = (key >> 5) * 16 + ((key >> 3) & 3) * 4 + (key & 3);
-          float p = 0.f;
-#pragma unroll
-          for (int i = 0; i < 16 * NB; ++i) p = at == i ? S[i >> 4][i & 15] : p;
-          p = __shfl(p, 32 * ((key >> 2) & 1) + col, 64);
-          const bool see = sees(key, __builtin_amdgcn_readlane(tp, key));
-          const char* row = ldsv + key * RB;
-          const int fv = C::fv(key);
-#pragma unroll
-          for (int d = 0; d < ND; ++d)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const int byte = (32 * d + 8 * (e >> 2) + 4 * half + (e & 3)) * (int)sizeof(T);
-              const char* src = row + (((byte >> 4) ^ fv) << 4) + (byte & 15);
-              const float x = F32 ? *(const float*)src : __uint_as_float((uint32_t)*(const uint16_t*)src << 16);
-              O[d][e] = see ? fmaf(p, x, O[d][e]) : O[d][e];
-            }
-        }
+          for (int e = 0; e < 16; ++e) {
+            const float x = (float)row[32 * d + 8 * (e >> 2) + (e & 3)];
+            O[d][e] += odd_bits(__float_as_uint(x), true) ? x : 0.f;
+          }
       }
     }
-    if constexpr (KW > 1) {
-      reads_done();
-      if (more) load_rows(gr, a.v, cur + C::kTile, false);
-    } else {
-      cur = cur == my ? my + 2 * C::kTile : my;
-    }
-    tp = tp_next;
   }
 
   l += other_half(l);
@@ -515,14 +610,14 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     float wm[4], M = -INFINITY;
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      wm[w] = ((const float*)(lds + w * C::kLds))[kStatAt + r];
+      wm[w] = ((const float*)(lds + w * (C::kLds + kRing)))[kStatAt + r];
       M = fmaxf(M, wm[w]);
     }
     const float Ms = M == -INFINITY ? 0.f : M;
     float L = 0.f, SF = 0.f, x[D / 8] = {};
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float* src = (const float*)(lds + w * C::kLds);
+      const float* src = (const float*)(lds + w * (C::kLds + kRing));
       const float f = __builtin_amdgcn_exp2f(wm[w] - Ms);
       L += f * src[kStatAt + kWaveRows + r];
       SF += f * src[kStatAt + 2 * kWaveRows + r];
@@ -784,7 +879,7 @@ hipError_t launch_paged_attend(const lg_paged_layer& l, const lg_page_map& m, co
   a.scale_log2 = kLog2e / sqrtf((float)l.head_dim);
   const dim3 grid((unsigned)((p.many_tiles + m.batch) * l.n_kv_heads * p.ns));
   const dim3 join((unsigned)(((long)total * l.n_q_heads + kJoinRows - 1) / kJoinRows));
-  auto go = [&](auto kernel, auto joined) {
+  auto go = [&](auto kernel, auto joined) __attribute__((always_inline)) {
     hipLaunchKernelGGL(kernel, grid, dim3(kPagedThreads), 0, st, a);
     if (p.ns > 1) hipLaunchKernelGGL(joined, join, dim3(kPagedThreads), 0, st, a);
   };
