@@ -58,31 +58,35 @@ struct PagedAttendArgs {
   float scale_log2;
 };
 
-// Sizes of the team that shares a tile: the workgroup (KW = 1) or a wave (KW = 4).
+// Sizes of the team that shares a tile: the workgroup (KW = 1) or a wave (KW = 4, 8).
 //
 // A row of K or V in LDS is its 16-byte pieces in the order piece ^ f(row): the 16 rows whose pieces one read
 // of K takes, and the 4 rows (of 64 bytes) that a transposed read of V takes, then lie in different banks,
 // without padding. The rows a lane reads differ from its first one by multiples that leave f as it is, so the
 // exchange is one xor with a constant on its first address (tiles lie at multiples of 1024 bytes).
-template <typename T, int D, int KW>
+//
+// DV: the values of V that the workgroup forms outputs of, D or (KW = 8) half of them.
+template <typename T, int D, int KW, int DV = D>
 struct Team {
   static constexpr bool kF32 = sizeof(T) == 4;
-  static constexpr int kRowBytes = D * (int)sizeof(T);
-  static constexpr int kRowPieces = kRowBytes / 16;
+  static constexpr int kRowBytes = D * (int)sizeof(T), kRowBytesV = DV * (int)sizeof(T);
+  static constexpr int kRowPieces = kRowBytes / 16, kRowPiecesV = kRowBytesV / 16;
   static constexpr int kKeys = kF32 || KW > 1 ? 32 : 64;  // slots of a tile
   static constexpr int kThreads = KW > 1 ? 64 : kPagedThreads;
-  static constexpr int kPieces = kKeys * kRowPieces / kThreads;  // 16-byte pieces a thread, of K and of V
-  static constexpr int kLoadRows = 64 / kRowPieces;               // rows that a wave loads at once
+  static constexpr int kPieces = kKeys * kRowPieces / kThreads;  // 16-byte pieces a thread, of K ...
+  static constexpr int kPiecesV = kKeys * kRowPiecesV / kThreads;  // ... and of V
+  static constexpr int kLoadRows = 64 / kRowPieces, kLoadRowsV = 64 / kRowPiecesV;  // rows that a wave loads at once
   static constexpr int kWaveLoad = kKeys / (KW > 1 ? 1 : 4);      // rows of a tile that a wave loads
   static constexpr int kGroups = kWaveLoad > 16 ? kWaveLoad / 16 : 1;  // of 16 rows, each inside one page
-  static constexpr int kTile = kKeys * kRowBytes;
-  static constexpr int kBuffers = KW > 1 ? 1 : 2;
-  // the join of KW = 4: a wave's O as [row][D + 4] and its m, l, suffix sums
-  static constexpr int kJoin = KW > 1 ? kWaveRows * (D + 4) * 4 + 3 * kWaveRows * 4 : 0;
-  static constexpr int kLds = 2 * kTile * kBuffers > kJoin ? 2 * kTile * kBuffers : (kJoin + 511) & ~511;
+  static constexpr int kTile = kKeys * kRowBytes, kTileV = kKeys * kRowBytesV;
+  static constexpr int kBuffer = kTile + kTileV;
+  // the join of KW > 1: a wave's O as [row][DV + 4] and its m, l, suffix sums
+  static constexpr int kJoin = KW > 1 ? kWaveRows * (DV + 4) * 4 + 3 * kWaveRows * 4 : 0;
+  static constexpr int kTiles = kBuffer * (KW > 1 ? 1 : 2);
+  static constexpr int kLds = kTiles > kJoin ? kTiles : (kJoin + 511) & ~511;
   static __device__ __forceinline__ int fk(int row) { return kF32 || D == 128 ? row & 15 : (row >> 1) & 7; }
   static __device__ __forceinline__ int fv(int row) {
-    return kF32 ? 8 * ((row >> 2) & 1) : D == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
+    return kF32 ? 8 * ((row >> 2) & 1) : DV == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
   }
 };
 
@@ -92,7 +96,12 @@ constexpr int kRing = 3 * 512;
 template <typename T, int D>
 constexpr int paged_lds() {
   constexpr int many = Team<T, D, 1>::kLds + 4 * kRing, few = 4 * (Team<T, D, 4>::kLds + kRing);
-  return (many > few ? many : few) + 16;
+  return (many > few ? many : few) + 4 * 4;  // and the flags of make_finite
+}
+
+template <typename T, int D, int KW, int DV>
+constexpr int few_lds() {
+  return KW * (Team<T, D, KW, DV>::kLds + kRing) + 4 * KW;
 }
 
 // The value of lane ^ 32.
@@ -155,6 +164,9 @@ __device__ __forceinline__ void schedule_scores() {
   __builtin_amdgcn_sched_group_barrier(0x008, 8, 0);
 }
 
+template <int N>
+using Num = std::integral_constant<int, N>;
+
 // What a workgroup attends with: its rows, and the slots that any of them may see.
 struct Job {
   int b, h;         // sequence, KV head
@@ -166,13 +178,15 @@ struct Job {
   int tile0;        // first tile of the rest
   int t_begin, t_end;  // this split's share of the sink_tiles + rest tiles
   int split;
+  int d0;  // first of the DV values of V
 };
 
-template <typename T, int D, int KW>
-__device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& job, char* lds) {
-  using C = Team<T, D, KW>;
+// flags: in LDS, one a team (see make_finite).
+template <typename T, int D, int KW, int DV>
+__device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& job, char* lds, int32_t* flags) {
+  using C = Team<T, D, KW, DV>;
   constexpr bool F32 = C::kF32;
-  constexpr int NK = C::kKeys, NB = NK / 32, ND = D / 32, NP = C::kPieces, RB = C::kRowBytes;
+  constexpr int NK = C::kKeys, NB = NK / 32, ND = DV / 32, RB = C::kRowBytes, RBV = C::kRowBytesV;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int half = lane >> 5, col = lane & 31;
   char* const my = KW > 1 ? lds + wave * (C::kLds + kRing) : lds;
@@ -228,7 +242,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
   // p of a row loads piece p ^ f(row). Slots behind last_slot read as last_slot and slots of missing pages
   // as page 0: no row sees them.
   int32_t* const ring = (int32_t*)(my + C::kLds + (KW > 1 ? 0 : wave * kRing));
-  int32_t* const odd = (int32_t*)(lds + paged_lds<T, D>() - 16) + (KW > 1 ? wave : 0);  // see make_finite
+  int32_t* const odd = flags + (KW > 1 ? wave : 0);
   auto look = [&](int t, int32_t* __restrict__ to) __attribute__((always_inline)) {
     const int s = min(slot_of(min(t, t_end - 1)) + (lane & (NK - 1)), last_slot);
     load_lds4(table + (s >> m.shift), to);
@@ -236,7 +250,6 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
   };
   // The position of the lane's slot, kHidden without a page.
   auto place = [&](const int32_t* at) __attribute__((always_inline)) { return is_page(m, at[lane]) ? at[64 + lane] : kHidden; };
-  const int lrow = lane / C::kRowPieces, piece = lane % C::kRowPieces;
   const int load0 = KW > 1 ? 0 : wave * C::kWaveLoad;  // the wave's first row of a tile
   struct Groups {
     size_t at[C::kGroups];  // bytes of the group's first row in k and v
@@ -256,29 +269,39 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     }
     return gr;
   };
-  // Rows of a tile to LDS at `to` + off. A group with all its rows (all but the last of a sequence) needs
-  // one offset a lane; the rest is in the instruction and an exclusive or.
-  const int lk = lrow * RB + 16 * (piece ^ C::fk(load0 | lrow)), lv = lrow * RB + 16 * (piece ^ C::fv(load0 | lrow));
-  auto load_rows = [&](const Groups& gr, const void* pages, char* to, int off, bool is_k) __attribute__((always_inline)) {
+  // Rows of a tile's K or V to LDS at `to` + off. A group with all its rows (all but the last of a sequence)
+  // needs one offset a lane; the rest is in the instruction and an exclusive or.
+  auto load_part = [&](const Groups& gr, const char* pages, char* to, int off, auto pieces, auto n, auto stride,
+                       auto f) __attribute__((always_inline)) {
+    constexpr int kRow = decltype(pieces)::value, kN = decltype(n)::value, kStep = 64 / kRow;
+    const int lrow = lane / kRow, piece = lane % kRow;
+    const int first = lrow * RB + 16 * (piece ^ f(load0 | lrow));
 #pragma unroll
     for (int i = 0; i < C::kGroups; ++i) {
-      const char* base = (const char*)pages + gr.at[i];
+      const char* base = pages + gr.at[i];
       const bool whole = gr.most[i] >= 15;
 #pragma unroll
-      for (int u = i * NP / C::kGroups; u < (i + 1) * NP / C::kGroups; ++u) {
-        const int up = u * C::kLoadRows, row = (load0 + up) | lrow;
-        unsigned at = (is_k ? lk ^ (16 * C::fk(up)) : lv ^ (16 * C::fv(up))) + ((load0 + up) & 15) * RB;
-        if (!whole)
-          at = (unsigned)(min(row & 15, gr.most[i]) * RB + 16 * (piece ^ (is_k ? C::fk(row) : C::fv(row))));
-        load_lds(base, at, to + off + (load0 + up) * RB);
+      for (int u = i * kN / C::kGroups; u < (i + 1) * kN / C::kGroups; ++u) {
+        const int up = u * kStep, row = (load0 + up) | lrow;
+        unsigned at = (first ^ (16 * f(up))) + ((load0 + up) & 15) * RB;
+        if (!whole) at = (unsigned)(min(row & 15, gr.most[i]) * RB + 16 * (piece ^ f(row)));
+        load_lds(base, at, to + off + (load0 + up) * decltype(stride)::value);
       }
     }
+  };
+  auto load_k = [&](const Groups& gr, char* to, int off) __attribute__((always_inline)) {
+    load_part(gr, (const char*)a.k, to, off, Num<C::kRowPieces>{}, Num<C::kPieces>{}, Num<RB>{},
+              [](int row) { return C::fk(row); });
+  };
+  auto load_v = [&](const Groups& gr, char* to, int off) __attribute__((always_inline)) {
+    load_part(gr, (const char*)a.v + job.d0 * sizeof(T), to, off, Num<C::kRowPiecesV>{}, Num<C::kPiecesV>{}, Num<RBV>{},
+              [](int row) { return C::fv(row); });
   };
 
   // The lane's first addresses in a tile (see Team).
   const int kx = col * RB + 16 * ((F32 ? half * (C::kRowPieces / 2) : half) ^ C::fk(col));
-  const int vx = F32 ? 4 * half * RB + 16 * ((col >> 2) ^ C::fv(4 * half)) + 4 * (col & 3)
-                     : (4 * half + ((lane & 15) >> 2)) * RB +
+  const int vx = F32 ? 4 * half * RBV + 16 * ((col >> 2) ^ C::fv(4 * half)) + 4 * (col & 3)
+                     : (4 * half + ((lane & 15) >> 2)) * RBV +
                            16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ C::fv((lane & 15) >> 2)) +
                            8 * (lane & 1);
 
@@ -373,7 +396,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
   // Puts 0 in the place of what is not finite in V of a tile (in LDS), and says so in *odd. With KW = 1 other waves
   // may read the tile meanwhile: they find a value or its 0, and the pass behind the loop adds the value.
   auto make_finite = [&](char* v) __attribute__((always_inline)) {
-    for (int i = lane; i < C::kTile / 16; i += 64) {
+    for (int i = lane; i < C::kTileV / 16; i += 64) {
       u32x4_t x = *(const u32x4_t*)(v + 16 * i);
       if (odd_bits(x[0], F32) || odd_bits(x[1], F32) || odd_bits(x[2], F32) || odd_bits(x[3], F32)) {
 #pragma unroll
@@ -398,7 +421,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
       for (int i = 0; i < 16; ++i)
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-          const float x = *(const float*)(from + ((v + vx) ^ (128 * d)) + (8 * (i >> 2) + (i & 3)) * RB);
+          const float x = *(const float*)(from + ((v + vx) ^ (128 * d)) + (8 * (i >> 2) + (i & 3)) * RBV);
           O[d] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, P[i], O[d], 0, 0, 0);
         }
     } else {
@@ -410,10 +433,10 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
         // a 16-lane group reads 4 keys x 16 values and gets them transposed: lane = value
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
-          const char* at = from + ((v + vx) ^ (64 * d)) + 16 * s * RB;
+          const char* at = from + ((v + vx) ^ (64 * d)) + 16 * s * RBV;
           const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at);
           const i16x4 hi =
-              __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(at + 8 * RB));
+              __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)(at + 8 * RBV));
           const u32x2_t x = __builtin_bit_cast(u32x2_t, lo), y = __builtin_bit_cast(u32x2_t, hi);
           const u32x4_t z = {x[0], x[1], y[0], y[1]};
           O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, z), __builtin_bit_cast(bf16x8, p),
@@ -422,10 +445,10 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
       }
     }
   };
-  constexpr int kBlock = 32 * RB;  // bytes of 32 keys
+  constexpr int kBlock = 32 * RB, kBlockV = 32 * RBV;  // bytes of 32 keys
 
   // KW = 1: two buffers and one barrier a tile: a wave's loads have landed before it, so all have behind it, and
-  // what the loads behind it fill has been read. KW = 4: one buffer; K of the next tile is asked for when the
+  // what the loads behind it fill has been read. KW > 1: one buffer; K of the next tile is asked for when the
   // scores are formed, V when the product is, and the waits count the loads that may be on their way behind
   // those needed (loads land in order; others among them only make a wait longer). The tile functions take
   // what they fill and what they read as pointers that do not alias: the compiler would make every read wait for
@@ -437,17 +460,17 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     look(t_first, ring);
     wait_loads<0>();
     const Groups gr = groups(t_first, ring);
-    load_rows(gr, a.k, my, 0, true);
+    load_k(gr, my, 0);
     look(t_first + step, ring + 128);
-    load_rows(gr, a.v, my, C::kTile, false);
+    load_v(gr, my, C::kTile);
   }
   if constexpr (KW == 1) {
     auto tile = [&](int t, int at, const char* __restrict__ from, char* __restrict__ to, const Groups& gr,
                     int32_t* __restrict__ ring_to) __attribute__((always_inline)) {
-      const int other = 2 * C::kTile - at;
+      const int other = C::kBuffer - at;
       if (t + 1 < t_end) {
-        load_rows(gr, a.k, to, other, true);
-        load_rows(gr, a.v, to, other + C::kTile, false);
+        load_k(gr, to, other);
+        load_v(gr, to, other + C::kTile);
       }
       look(t + 2, ring_to);
       if (idle || s0 > slot_hi) return;
@@ -474,7 +497,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
       product(from, at + C::kTile, S);
       if constexpr (NB > 1) {
         sum += weights(S1);
-        product(from, at + C::kTile + kBlock, S1);
+        product(from, at + C::kTile + kBlockV, S1);
       }
       l += sum;
       sfx += how == kAll ? sum : 0.f;
@@ -486,12 +509,12 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
       const Groups gr = groups(t + 1, ring + 128 * n1);
       tp = place(ring + 128 * n);
       s0 = slot_of(t);
-      tile(t, (t - t_first & 1) * 2 * C::kTile, my, my, gr, ring + 128 * n2);
+      tile(t, ((t - t_first) & 1) * C::kBuffer, my, my, gr, ring + 128 * n2);
     }
   } else {
     auto behind_scores = [&](int t, bool more, const Groups& gr, f32x16& S, const char* __restrict__ from,
                              char* __restrict__ to, int32_t* __restrict__ ring_to) __attribute__((always_inline)) {
-      if (more) load_rows(gr, a.k, to, 0, true);
+      if (more) load_k(gr, to, 0);
       look(t + 2 * KW, ring_to);
       masked = is_masked();
       const int how = suffix_of();
@@ -502,7 +525,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
       l += sum;
       sfx += how == kAll ? sum : 0.f;
       if (more)
-        wait_loads<NP>();  // V is here; K of the next tile may be on its way
+        wait_loads<C::kPieces>();  // V is here; K of the next tile may be on its way
       else
         wait_loads<0>();
       if (masked) make_finite(const_cast<char*>(from) + C::kTile);
@@ -510,7 +533,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     };
     for (int t = t_first, n = 0; t < t_end; t += KW, n = n == 2 ? 0 : n + 1) {
       const bool more = t + KW < t_end;
-      wait_loads<NP>();  // K is here; V may be on its way
+      wait_loads<C::kPiecesV>();  // K is here; V may be on its way
       const int n1 = n == 2 ? 0 : n + 1, n2 = n1 == 2 ? 0 : n1 + 1;
       const Groups gr = groups(t + KW, ring + 128 * n1);
       tp = place(ring + 128 * n);
@@ -520,7 +543,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
       reads_done();
       behind_scores(t, more, gr, S, my, my, ring + 128 * n2);
       reads_done();
-      if (more) load_rows(gr, a.v, my, C::kTile, false);
+      if (more) load_v(gr, my, C::kTile);
     }
     wait_loads<0>();
   }
@@ -538,7 +561,8 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
         const int page = table[j >> m.shift];
         if (!is_page(m, page) || !sees(key, pos[j])) continue;
         const T* row = (const T*)a.v +
-                       ((((size_t)page * a.Hkv + job.h) << m.shift) + (j & ((1 << m.shift) - 1))) * D + 4 * half;
+                       ((((size_t)page * a.Hkv + job.h) << m.shift) + (j & ((1 << m.shift) - 1))) * D +
+                       job.d0 + 4 * half;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
@@ -589,73 +613,68 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
         raise_conf(a.conf + job.b, mass);
     }
   } else {
-    // Join the four waves: their numerators and statistics through LDS, 8 threads a row.
+    // Join the waves: their numerators and statistics through LDS, 2 KW threads a row.
+    constexpr int kStat = kWaveRows * (DV + 4), kParts = 2 * KW, kChunks = DV / (4 * kParts);
     float* const num = (float*)my;
-    float* const st = num + kWaveRows * (D + 4);
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        *(f32x4*)(num + col * (D + 4) + 32 * d + 8 * i + 4 * half) =
+        *(f32x4*)(num + col * (DV + 4) + 32 * d + 8 * i + 4 * half) =
             f32x4{O[d][4 * i], O[d][4 * i + 1], O[d][4 * i + 2], O[d][4 * i + 3]};
     if (half == 0) {
-      st[col] = mx;
-      st[kWaveRows + col] = l;
-      st[2 * kWaveRows + col] = sfx;
+      num[kStat + col] = mx;
+      num[kStat + kWaveRows + col] = l;
+      num[kStat + 2 * kWaveRows + col] = sfx;
     }
     __syncthreads();
-    const int r = tid >> 3, part = tid & 7;
+    const int r = tid / kParts, part = tid % kParts;
     if (job.row0 + r >= job.rows) return;
-    constexpr int kStatAt = kWaveRows * (D + 4);
-    float wm[4], M = -INFINITY;
+    float wm[KW], M = -INFINITY;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      wm[w] = ((const float*)(lds + w * (C::kLds + kRing)))[kStatAt + r];
+    for (int w = 0; w < KW; ++w) {
+      wm[w] = ((const float*)(lds + w * (C::kLds + kRing)))[kStat + r];
       M = fmaxf(M, wm[w]);
     }
     const float Ms = M == -INFINITY ? 0.f : M;
-    float L = 0.f, SF = 0.f, x[D / 8] = {};
+    float L = 0.f, SF = 0.f;
+    f32x4 x[kChunks] = {};
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < KW; ++w) {
       const float* src = (const float*)(lds + w * (C::kLds + kRing));
       const float f = __builtin_amdgcn_exp2f(wm[w] - Ms);
-      L += f * src[kStatAt + kWaveRows + r];
-      SF += f * src[kStatAt + 2 * kWaveRows + r];
+      L += f * src[kStat + kWaveRows + r];
+      SF += f * src[kStat + 2 * kWaveRows + r];
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const f32x4 y = *(const f32x4*)(src + r * (D + 4) + 32 * i + 4 * part);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[4 * i + e] += f * y[e];
-      }
+      for (int i = 0; i < kChunks; ++i) x[i] += f * *(const f32x4*)(src + r * (DV + 4) + 4 * (kParts * i + part));
     }
     const int tk = (job.row0 + r) / a.G, gg = job.row0 + r - tk * a.G;
     const size_t row = (size_t)(job.first + tk) * a.Hq + job.h * a.G + gg;
+    const bool first = part == 0 && job.d0 == 0;  // the row's statistics
     if (a.ns > 1) {
       const size_t at = (size_t)job.split * a.total * a.Hq + row;
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-        *(f32x4*)(a.po + at * D + 32 * i + 4 * part) = f32x4{x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]};
-      if (part == 0) *(f32x4*)(a.pml + at * 4) = f32x4{M, L, SF, 0.f};
+      for (int i = 0; i < kChunks; ++i) *(f32x4*)(a.po + at * D + job.d0 + 4 * (kParts * i + part)) = x[i];
+      if (first) *(f32x4*)(a.pml + at * 4) = f32x4{M, L, SF, 0.f};
       return;
     }
     const float inv = 1.f / L;
-    T* dst = (T*)a.out + row * D;
+    T* dst = (T*)a.out + row * D + job.d0;
 #pragma unroll
-    for (int i = 0; i < D / 32; ++i) {
-      float y[4];
+    for (int i = 0; i < kChunks; ++i) {
+      f32x4 y;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = L == 0.f ? 0.f : x[4 * i + e] * inv;
+      for (int e = 0; e < 4; ++e) y[e] = L == 0.f ? 0.f : x[i][e] * inv;
       if constexpr (F32)
-        *(f32x4*)(dst + 32 * i + 4 * part) = f32x4{y[0], y[1], y[2], y[3]};
+        *(f32x4*)(dst + 4 * (kParts * i + part)) = y;
       else
-        *(u32x2_t*)(dst + 32 * i + 4 * part) = u32x2_t{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+        *(u32x2_t*)(dst + 4 * (kParts * i + part)) = u32x2_t{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
     }
-    if (part == 0) {
+    if (first) {
       a.lse[row] = L == 0.f ? -INFINITY : kLn2 * (M + __builtin_amdgcn_logf(L));
       const float mass = L == 0.f ? 0.f : SF * inv;
       if (a.suffix != nullptr) a.suffix[row] = mass;
-      if (a.conf != nullptr && tk == job.rows / a.G - 1)
-        raise_conf(a.conf + job.b, mass);
+      if (a.conf != nullptr && tk == job.rows / a.G - 1) raise_conf(a.conf + job.b, mass);
     }
   }
 }
@@ -682,12 +701,30 @@ __device__ __forceinline__ void job_tiles(const PagedAttendArgs& a, Job& job, in
   job.t_end = (int)((long long)n * (split + 1) / a.ns);
 }
 
+// A sequence of at most 32 query rows: false if it has none, more, or is refused.
+__device__ __forceinline__ bool few_job(const PagedAttendArgs& a, Job& job, int b, bool first) {
+  const Chunk c = chunk_of(a.q_start, b, a.total);
+  job.base = a.base[b];
+  if (c.n == 0) return false;
+  if (job.base < 0 || c.n > a.max_chunk || job.base > a.map.cap - c.n) {  // refused
+    if (a.conf != nullptr && first && threadIdx.x == 0) a.conf[b] = NAN;
+    return false;
+  }
+  if ((long long)c.n * a.G > kWaveRows) return false;
+  job.b = b;
+  job.first = c.first;
+  job.rows = c.n * a.G;
+  job.row0 = 0;
+  return true;
+}
+
 // Grid: (Hkv, ns, many_tiles + B), flattened with the KV head fastest: the workgroups of one head of one
 // sequence are Hkv apart, so with 8 heads (the XCDs are dealt workgroups in turn) they share an L2. The
 // tiles of many rows come first, the last of a sequence (the longest) before the others.
 template <typename T, int D>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend(PagedAttendArgs a) {
   __shared__ __align__(16) char lds[paged_lds<T, D>()];
+  int32_t* const flags = (int32_t*)(lds + paged_lds<T, D>() - 16);
   const int per = a.Hkv * a.ns;
   const int unit = blockIdx.x / per, rest = blockIdx.x % per;
   Job job;
@@ -696,11 +733,14 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend(PagedAttendArgs
   const int lane = threadIdx.x & 63;
   if (unit < a.many_tiles) {
     // the sequence of this tile: tiles of sequences with more than 32 rows, counted 64 sequences at a time
-    int left = unit, b = -1, tiles = 0;
-    for (int b0 = 0; b0 < a.map.B; b0 += 64) {
+    int left = unit, tiles = 0, k = 0, b0 = 0, base = -1;
+    Chunk c = {0, 0};
+    for (;; b0 += 64) {
+      if (b0 >= a.map.B) return;
       int n = 0;
       if (b0 + lane < a.map.B) {
-        const Chunk c = chunk_of(a.q_start, b0 + lane, a.total);
+        c = chunk_of(a.q_start, b0 + lane, a.total);
+        base = a.base[b0 + lane];
         if (c.n <= a.max_chunk && (long long)c.n * a.G > kWaveRows) n = (int)(((long long)c.n * a.G + kManyRows - 1) / kManyRows);
       }
       int inc = n;
@@ -711,72 +751,105 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend(PagedAttendArgs
       }
       const unsigned long long over = __ballot(inc > left);
       if (over != 0) {
-        const int k = __builtin_ctzll(over);
+        k = __builtin_ctzll(over);
         tiles = __builtin_amdgcn_readlane(n, k);
         left -= __builtin_amdgcn_readlane(inc, k) - tiles;
-        b = b0 + k;
         break;
       }
       left -= __builtin_amdgcn_readlane(inc, 63);
     }
-    if (b < 0) return;
-    const Chunk c = chunk_of(a.q_start, b, a.total);
-    job.b = b;
-    job.first = c.first;
-    job.rows = c.n * a.G;
+    const int n = __builtin_amdgcn_readlane(c.n, k);
+    job.b = b0 + k;
+    job.first = __builtin_amdgcn_readlane(c.first, k);
+    job.rows = n * a.G;
     job.row0 = (tiles - 1 - left) * kManyRows;
-    job.base = a.base[b];
-    if (job.base < 0 || job.base > a.map.cap - c.n) return;
+    job.base = __builtin_amdgcn_readlane(base, k);
+    if (job.base < 0 || job.base > a.map.cap - n) return;
     job_tiles<Team<T, D, 1>::kKeys>(a, job, kManyRows, split);
-    paged_body<T, D, 1>(a, job, lds);
+    job.d0 = 0;
+    paged_body<T, D, 1, D>(a, job, lds, flags);
     return;
   }
-  const int b = unit - a.many_tiles;
-  const Chunk c = chunk_of(a.q_start, b, a.total);
-  job.base = a.base[b];
-  if (c.n == 0) return;
-  if (job.base < 0 || c.n > a.max_chunk || job.base > a.map.cap - c.n) {  // refused
-    if (a.conf != nullptr && rest == 0 && threadIdx.x == 0) a.conf[b] = NAN;
-    return;
+  if (few_job(a, job, unit - a.many_tiles, rest == 0)) {
+    job_tiles<Team<T, D, 4>::kKeys>(a, job, kWaveRows, split);
+    job.d0 = 0;
+    paged_body<T, D, 4, D>(a, job, lds, flags);
   }
-  if ((long long)c.n * a.G > kWaveRows) return;
-  job.b = b;
-  job.first = c.first;
-  job.rows = c.n * a.G;
-  job.row0 = 0;
-  job_tiles<Team<T, D, 4>::kKeys>(a, job, kWaveRows, split);
-  paged_body<T, D, 4>(a, job, lds);
 }
 
-// Joins the splits of a row: a wave per query row of a token.
+// A step without sequences of more than 32 query rows. KW waves a workgroup (8 where LDS holds their tiles), so
+// a sequence's slots are swept by as many loads as the memory needs on their way with one workgroup a CU.
+// DV < D: two workgroups a KV head, each with all of K and half of V, in place of a split of the slots: no
+// second launch to join them, and K comes to the second from the L2 of their XCD (they are 8 workgroups apart).
+// Grid: (Hkv, ns, B) flattened into units; with two halves, groups of 8 units' first halves, then their second.
+template <typename T, int D, int KW, int DV>
+__global__ __launch_bounds__(64 * KW) void paged_few(PagedAttendArgs a) {
+  __shared__ __align__(16) char lds[few_lds<T, D, KW, DV>()];
+  const unsigned per = (unsigned)(a.Hkv * a.ns);
+  unsigned unit = blockIdx.x;
+  Job job;
+  job.d0 = 0;
+  if constexpr (DV < D) {
+    const unsigned group = unit / 16 * 8, in = unit % 16, size = min(8u, per * a.map.B - group);
+    unit = group + in % size;
+    job.d0 = in / size * DV;
+  }
+  const unsigned b = unit / per, x = unit % per;
+  job.h = x % a.Hkv;
+  if (!few_job(a, job, b, x == 0 && job.d0 == 0)) return;
+  job_tiles<32>(a, job, kWaveRows, x / a.Hkv);
+  paged_body<T, D, KW, DV>(a, job, lds, (int32_t*)(lds + few_lds<T, D, KW, DV>() - 4 * KW));
+}
+
+// Joins the splits of a row: a wave per query row of a token. What it reads of the partials does not depend on the
+// sequence (rows of no sequence hold anything), so all its loads are on their way at once: a lane per
+// split for the statistics, a lane per D / 64 values for the outputs.
 constexpr int kJoinRows = kPagedThreads / 64;
+constexpr int kMaxNs = 64;
+constexpr int kJoinAhead = 8;  // splits whose outputs are loaded together
 
 template <typename T, int D>
 __global__ __launch_bounds__(kPagedThreads) void paged_join(PagedAttendArgs a) {
+  constexpr int E = D / 64;
+  typedef float fE __attribute__((ext_vector_type(E)));
   const long long row = (long long)blockIdx.x * kJoinRows + (threadIdx.x >> 6);
   const long long rows = (long long)a.total * a.Hq;
   if (row >= rows) return;
   const int r = (int)(row / a.Hq), lane = threadIdx.x & 63;
+  const f32x4 st = lane < a.ns ? *(const f32x4*)(a.pml + (lane * rows + row) * 4) : f32x4{-INFINITY, 0.f, 0.f, 0.f};
+  fE y[kJoinAhead];
+  auto load = [&](int s0) {
+#pragma unroll
+    for (int i = 0; i < kJoinAhead; ++i)
+      if (s0 + i < a.ns) y[i] = *(const fE*)(a.po + ((s0 + i) * rows + row) * D + lane * E);
+  };
+  load(0);
   const int b = seq_of_row(a.q_start, a.map.B, r);
   if (b >= a.map.B) return;
   const Chunk c = chunk_of(a.q_start, b, a.total);
   const int base = a.base[b];
   if (r < c.first || r >= c.first + c.n || c.n > a.max_chunk || base < 0 || base > a.map.cap - c.n) return;
-  float M = -INFINITY;
-  for (int s = 0; s < a.ns; ++s) M = fmaxf(M, a.pml[(s * rows + row) * 4]);
-  const float Ms = M == -INFINITY ? 0.f : M;
-  float L = 0.f, SF = 0.f, x[D / 64] = {};
-  for (int s = 0; s < a.ns; ++s) {
-    const f32x4 st = *(const f32x4*)(a.pml + (s * rows + row) * 4);
-    const float f = __builtin_amdgcn_exp2f(st[0] - Ms);
-    L += f * st[1];
-    SF += f * st[2];
+  float M = st[0], L, SF;
 #pragma unroll
-    for (int e = 0; e < D / 64; ++e) x[e] += f * a.po[(s * rows + row) * D + lane * (D / 64) + e];
+  for (int o = 1; o < 64; o <<= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
+  const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[0] - M);
+  L = f * st[1];
+  SF = f * st[2];
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    L += __shfl_xor(L, o, 64);
+    SF += __shfl_xor(SF, o, 64);
+  }
+  fE x = {};
+  for (int s0 = 0; s0 < a.ns; s0 += kJoinAhead) {
+    if (s0 > 0) load(s0);
+#pragma unroll
+    for (int i = 0; i < kJoinAhead; ++i)
+      if (s0 + i < a.ns) x += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s0 + i)) * y[i];
   }
   const float inv = 1.f / L;
 #pragma unroll
-  for (int e = 0; e < D / 64; ++e) ((T*)a.out)[row * D + lane * (D / 64) + e] = (T)(L == 0.f ? 0.f : x[e] * inv);
+  for (int e = 0; e < E; ++e) ((T*)a.out)[row * D + lane * E + e] = (T)(L == 0.f ? 0.f : x[e] * inv);
   if (lane == 0) {
     a.lse[row] = L == 0.f ? -INFINITY : kLn2 * (M + __builtin_amdgcn_logf(L));
     const float mass = L == 0.f ? 0.f : SF * inv;
@@ -790,24 +863,42 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join(PagedAttendArgs a) {
 // ------------------------------------------------------------------------------------------
 struct PagedPlan {
   long many_tiles;  // upper bound over the chunks that `total` rows can be
-  int ns;
+  int ns;           // splits of a row's slots
+  int halves;       // workgroups that share a row's output values (paged_few)
+  bool few;         // paged_few
 };
+
+// Workgroups for the split of a launch without long chunks: one a CU.
+constexpr long kFewTarget = 256;
 
 static PagedPlan paged_plan(const lg_paged_layer& l, const lg_page_map& m, long total, long max_chunk) {
   const long G = l.n_q_heads / l.n_kv_heads;
   PagedPlan p;
   p.many_tiles = 0;
-  if (max_chunk * G > kWaveRows && total * G > kWaveRows) {
-    // a sequence of n rows has at most n / 128 + 1 tiles, and more than 32 rows
-    p.many_tiles = total * G / kManyRows;
-    const long seqs = total * G / (kWaveRows + 1);
-    p.many_tiles += seqs < m.batch ? seqs : m.batch;
-  }
-  const long units = (p.many_tiles + m.batch) * l.n_kv_heads;
+  p.halves = 1;
+  p.few = max_chunk * G <= kWaveRows;
   const long cap = (long)m.max_pages * m.page_size;
-  long ns = (kPagedTarget + units - 1) / units;
   const long most = (cap + kMinSplitSlots - 1) / kMinSplitSlots;
+  long ns;
+  if (p.few) {
+    const long units = (long)m.batch * l.n_kv_heads;
+    ns = kFewTarget / units;  // more than one a CU would run in two rounds
+    if (l.head_dim == 128 && ns == 2) {
+      ns = 1;
+      p.halves = 2;
+    }
+  } else {
+    if (total * G > kWaveRows) {
+      // a sequence of n rows has at most n / 128 + 1 tiles, and more than 32 rows
+      p.many_tiles = total * G / kManyRows;
+      const long seqs = total * G / (kWaveRows + 1);
+      p.many_tiles += seqs < m.batch ? seqs : m.batch;
+    }
+    const long units = (p.many_tiles + m.batch) * l.n_kv_heads;
+    ns = (kPagedTarget + units - 1) / units;
+  }
   if (ns > most) ns = most;
+  if (ns > kMaxNs) ns = kMaxNs;
   p.ns = (int)(ns < 1 ? 1 : ns);
   return p;
 }
@@ -819,7 +910,7 @@ static size_t paged_need(const lg_paged_layer& l, const PagedPlan& p, long total
 // Workgroups of the launch (a grid holds fewer than 2^32 threads).
 long paged_attend_grid(const lg_paged_layer& l, const lg_page_map& m, int total, int max_chunk) {
   const PagedPlan p = paged_plan(l, m, total, max_chunk);
-  return (p.many_tiles + m.batch) * l.n_kv_heads * p.ns;
+  return (p.many_tiles + m.batch) * l.n_kv_heads * p.ns * p.halves;
 }
 
 size_t paged_attend_need(const lg_paged_layer& l, const lg_page_map& m, int total, int max_chunk) {
@@ -846,6 +937,21 @@ size_t paged_attend_bytes(const lg_paged_layer& l, const lg_page_map& m, int tot
     }
   }
   return align_up(most, 16);
+}
+
+template <typename T, int D>
+static void launch_typed(const PagedAttendArgs& a, const PagedPlan& p, dim3 grid, hipStream_t st) {
+  constexpr int KW = sizeof(T) == 4 && D == 128 ? 4 : 8;
+  if (!p.few)
+    hipLaunchKernelGGL((paged_attend<T, D>), grid, dim3(kPagedThreads), 0, st, a);
+  else if (p.halves == 1)
+    hipLaunchKernelGGL((paged_few<T, D, KW, D>), grid, dim3(64 * KW), 0, st, a);
+  else if constexpr (D == 128)
+    hipLaunchKernelGGL((paged_few<T, D, KW, D / 2>), grid, dim3(64 * KW), 0, st, a);
+  const long rows = (long)a.total * a.Hq;
+  if (p.ns > 1)
+    hipLaunchKernelGGL((paged_join<T, D>), dim3((unsigned)((rows + kJoinRows - 1) / kJoinRows)), dim3(kPagedThreads), 0,
+                       st, a);
 }
 
 hipError_t launch_paged_attend(const lg_paged_layer& l, const lg_page_map& m, const void* q, void* out,
@@ -877,18 +983,13 @@ hipError_t launch_paged_attend(const lg_paged_layer& l, const lg_page_map& m, co
   a.ns = p.ns;
   a.many_tiles = (int)p.many_tiles;
   a.scale_log2 = kLog2e / sqrtf((float)l.head_dim);
-  const dim3 grid((unsigned)((p.many_tiles + m.batch) * l.n_kv_heads * p.ns));
-  const dim3 join((unsigned)(((long)total * l.n_q_heads + kJoinRows - 1) / kJoinRows));
-  auto go = [&](auto kernel, auto joined) __attribute__((always_inline)) {
-    hipLaunchKernelGGL(kernel, grid, dim3(kPagedThreads), 0, st, a);
-    if (p.ns > 1) hipLaunchKernelGGL(joined, join, dim3(kPagedThreads), 0, st, a);
-  };
+  const dim3 grid((unsigned)((p.many_tiles + m.batch) * l.n_kv_heads * p.ns * p.halves));
   if (l.dtype == LG_BF16) {
-    if (l.head_dim == 128) go(paged_attend<__bf16, 128>, paged_join<__bf16, 128>);
-    else go(paged_attend<__bf16, 64>, paged_join<__bf16, 64>);
+    if (l.head_dim == 128) launch_typed<__bf16, 128>(a, p, grid, st);
+    else launch_typed<__bf16, 64>(a, p, grid, st);
   } else {
-    if (l.head_dim == 128) go(paged_attend<float, 128>, paged_join<float, 128>);
-    else go(paged_attend<float, 64>, paged_join<float, 64>);
+    if (l.head_dim == 128) launch_typed<float, 128>(a, p, grid, st);
+    else launch_typed<float, 64>(a, p, grid, st);
   }
   return hipGetLastError();
 }
