@@ -36,6 +36,7 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kWaveRows = 32;
@@ -331,27 +332,32 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     return fmaxf(x, other_half(x));
   };
 
-  // What a tile needs compared, the same in all lanes; tp: its positions, a lane per slot.
+  // What a tile needs compared, the same in all lanes. tp: its positions, a lane per slot; at: the wave's table
+  // entries and positions of it in LDS. In a masked tile the entries, not needed any more, become the slots' own
+  // bounds: a row sees slot j if bound_j > win and the slot is none behind its own. Both are read four slots
+  // at a time, as they lie in the accumulators' rows.
   int s0, tp;
+  int32_t* at;
   bool masked;
-  // position of accumulator row i of block nb, in the lane's half
-  auto pos_of = [&](int nb, int i) __attribute__((always_inline)) {
-    const int key = 32 * nb + 8 * (i >> 2) + (i & 3);
-    const int lo = __builtin_amdgcn_readlane(tp, key), hi = __builtin_amdgcn_readlane(tp, key + 4);
-    return half ? hi : lo;
-  };
-  auto sees = [&](int key, int pj) __attribute__((always_inline)) {
-    return s0 + key <= slot_q && pj != kHidden && (pj > win || a.window == 0 || pj < a.n_sink);
-  };
   auto is_masked = [&]() __attribute__((always_inline)) {
     const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
     return __ballot(tp == kHidden) != 0 || s0 + NK - 1 > slot_lo ||
            (a.window > 0 && p_first <= win_hi && p_last >= a.n_sink);
   };
+  auto four = [&](const int32_t* x, int nb, int i) __attribute__((always_inline)) {
+    return *(const i32x4*)(x + 32 * nb + 8 * i + 4 * half);
+  };
+  auto set_bounds = [&]() __attribute__((always_inline)) {
+    at[lane] = tp == kHidden ? INT32_MIN : a.window == 0 || tp < a.n_sink ? INT32_MAX : tp;
+  };
   auto mask = [&](f32x16& S, int nb) __attribute__((always_inline)) {
+    const int last = slot_q - s0 - 32 * nb - 4 * half;
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-      S[i] = sees(32 * nb + 8 * (i >> 2) + 4 * half + (i & 3), pos_of(nb, i)) ? S[i] : -INFINITY;
+    for (int i = 0; i < 4; ++i) {
+      const i32x4 bound = four(at, nb, i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) S[4 * i + j] = bound[j] > win && 8 * i + j <= last ? S[4 * i + j] : -INFINITY;
+    }
   };
   // The running maximum follows only when a score passes it by kSlack: weights are then at most 2^kSlack,
   // which costs no precision, and most tiles leave O as it is. A row goes by its own scores alone.
@@ -369,26 +375,27 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
         for (int i = 0; i < 16; ++i) O[d][i] *= f;
     }
   };
-  // The suffix's share of a tile: none, all, or slot by slot
+  // The suffix's share of a tile: none, all, or slot by slot (slots that are not seen have weight 0)
   enum { kNone, kAll, kSome };
   auto suffix_of = [&]() __attribute__((always_inline)) {
     if (a.suffix == nullptr && a.conf == nullptr) return (int)kNone;
     const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
-    return masked ? (int)kSome : p_last <= suf_lo ? (int)kNone : p_first > suf_hi ? (int)kAll : (int)kSome;
+    return p_last <= suf_lo ? (int)kNone : p_first > suf_hi ? (int)kAll : (int)kSome;
   };
-  auto weight = [&](float s) __attribute__((always_inline)) {
-    return __builtin_amdgcn_exp2f(fmaf(s, a.scale_log2, mx == -INFINITY ? 0.f : -mx));
-  };
-  auto add_suffix = [&](const f32x16& S, int nb) __attribute__((always_inline)) {
+  auto add_suffix = [&](const f32x16& P, int nb) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) sfx += pos_of(nb, i) > suf ? weight(S[i]) : 0.f;
+    for (int i = 0; i < 4; ++i) {
+      const i32x4 p = four(at + 64, nb, i);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sfx += p[j] > suf ? P[4 * i + j] : 0.f;
+    }
   };
   // S becomes the weights; returns their sum over the lane's half.
   auto weights = [&](f32x16& S) __attribute__((always_inline)) {
     float s4[4];
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      S[i] = weight(S[i]);
+      S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], a.scale_log2, mx == -INFINITY ? 0.f : -mx));
       s4[i & 3] = i < 4 ? S[i] : s4[i & 3] + S[i];
     }
     return (s4[0] + s4[1]) + (s4[2] + s4[3]);
@@ -465,9 +472,9 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     load_v(gr, my, C::kTile);
   }
   if constexpr (KW == 1) {
-    auto tile = [&](int t, int at, const char* __restrict__ from, char* __restrict__ to, const Groups& gr,
+    auto tile = [&](int t, int here, const char* __restrict__ from, char* __restrict__ to, const Groups& gr,
                     int32_t* __restrict__ ring_to) __attribute__((always_inline)) {
-      const int other = C::kBuffer - at;
+      const int other = C::kBuffer - here;
       if (t + 1 < t_end) {
         load_k(gr, to, other);
         load_v(gr, to, other + C::kTile);
@@ -475,39 +482,41 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
       look(t + 2, ring_to);
       if (idle || s0 > slot_hi) return;
       f32x16 S, S1;
-      scores(from, at, S);
+      scores(from, here, S);
       if constexpr (NB > 1) {
-        scores(from, at + kBlock, S1);
+        scores(from, here + kBlock, S1);
         schedule_scores();
       }
       masked = is_masked();
       const int how = suffix_of();
       if (masked) {
-        make_finite(const_cast<char*>(from) + at + C::kTile);
+        set_bounds();
+        make_finite(const_cast<char*>(from) + here + C::kTile);
         mask(S, 0);
         if constexpr (NB > 1) mask(S1, 1);
       }
       raise_max(NB > 1 ? fmaxf(top(S), top(S1)) : top(S));
+      // Without a branch up to the sums: the second block's exponentials beside the first one's product.
+      float sum = weights(S);
+      product(from, here + C::kTile, S);
+      if constexpr (NB > 1) {
+        sum += weights(S1);
+        product(from, here + C::kTile + kBlockV, S1);
+      }
+      l += sum;
+      sfx += how == kAll ? sum : 0.f;
       if (how == kSome) {
         add_suffix(S, 0);
         if constexpr (NB > 1) add_suffix(S1, 1);
       }
-      // From here on without a branch: the second block's exponentials beside the first one's product.
-      float sum = weights(S);
-      product(from, at + C::kTile, S);
-      if constexpr (NB > 1) {
-        sum += weights(S1);
-        product(from, at + C::kTile + kBlockV, S1);
-      }
-      l += sum;
-      sfx += how == kAll ? sum : 0.f;
     };
     for (int t = t_first, n = 0; t < t_end; ++t, n = n == 2 ? 0 : n + 1) {
       wait_loads<0>();
       __syncthreads();
       const int n1 = n == 2 ? 0 : n + 1, n2 = n1 == 2 ? 0 : n1 + 1;
       const Groups gr = groups(t + 1, ring + 128 * n1);
-      tp = place(ring + 128 * n);
+      at = ring + 128 * n;
+      tp = place(at);
       s0 = slot_of(t);
       tile(t, ((t - t_first) & 1) * C::kBuffer, my, my, gr, ring + 128 * n2);
     }
@@ -518,12 +527,15 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
       look(t + 2 * KW, ring_to);
       masked = is_masked();
       const int how = suffix_of();
-      if (masked) mask(S, 0);
+      if (masked) {
+        set_bounds();
+        mask(S, 0);
+      }
       raise_max(top(S));
-      if (how == kSome) add_suffix(S, 0);
       const float sum = weights(S);
       l += sum;
       sfx += how == kAll ? sum : 0.f;
+      if (how == kSome) add_suffix(S, 0);
       if (more)
         wait_loads<C::kPieces>();  // V is here; K of the next tile may be on its way
       else
@@ -536,7 +548,8 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
       wait_loads<C::kPiecesV>();  // K is here; V may be on its way
       const int n1 = n == 2 ? 0 : n + 1, n2 = n1 == 2 ? 0 : n1 + 1;
       const Groups gr = groups(t + KW, ring + 128 * n1);
-      tp = place(ring + 128 * n);
+      at = ring + 128 * n;
+      tp = place(at);
       s0 = slot_of(t);
       f32x16 S;
       scores(my, 0, S);
@@ -559,7 +572,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
       for (int key = 0; key < NK; ++key) {
         const int j = min(s0 + key, last_slot);
         const int page = table[j >> m.shift];
-        if (!is_page(m, page) || !sees(key, pos[j])) continue;
+        if (!is_page(m, page) || s0 + key > slot_q || (a.window > 0 && pos[j] <= win && pos[j] >= a.n_sink)) continue;
         const T* row = (const T*)a.v +
                        ((((size_t)page * a.Hkv + job.h) << m.shift) + (j & ((1 << m.shift) - 1))) * D +
                        job.d0 + 4 * half;
@@ -723,7 +736,7 @@ __device__ __forceinline__ bool few_job(const PagedAttendArgs& a, Job& job, int 
 // tiles of many rows come first, the last of a sequence (the longest) before the others.
 template <typename T, int D>
 __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend(PagedAttendArgs a) {
-  __shared__ __align__(16) char lds[paged_lds<T, D>()];
+  __shared__ __align__(512) char lds[paged_lds<T, D>()];
   int32_t* const flags = (int32_t*)(lds + paged_lds<T, D>() - 16);
   const int per = a.Hkv * a.ns;
   const int unit = blockIdx.x / per, rest = blockIdx.x % per;
@@ -784,7 +797,7 @@ __global__ __launch_bounds__(kPagedThreads, 2) void paged_attend(PagedAttendArgs
 // Grid: (Hkv, ns, B) flattened into units; with two halves, groups of 8 units' first halves, then their second.
 template <typename T, int D, int KW, int DV>
 __global__ __launch_bounds__(64 * KW) void paged_few(PagedAttendArgs a) {
-  __shared__ __align__(16) char lds[few_lds<T, D, KW, DV>()];
+  __shared__ __align__(512) char lds[few_lds<T, D, KW, DV>()];
   const unsigned per = (unsigned)(a.Hkv * a.ns);
   unsigned unit = blockIdx.x;
   Job job;
