@@ -128,11 +128,11 @@ _MP, _PP = ctypes.POINTER(PageMap), ctypes.POINTER(PagedLayer)
 _lib.lg_page_workspace.restype = _sz
 _lib.lg_page_workspace.argtypes = [_MP]
 _lib.lg_page_reserve.restype = ctypes.c_int
-_lib.lg_page_reserve.argtypes = [_MP, _i32, _PP, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.lg_page_reserve.argtypes = [_MP, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.lg_page_fork.restype = ctypes.c_int
 _lib.lg_page_fork.argtypes = [_MP, _vp, _vp, _sz, _vp]
 _lib.lg_page_compact.restype = ctypes.c_int
-_lib.lg_page_compact.argtypes = [_MP, _i32, _PP, _vp, _vp, _vp, _vp, _sz, _vp]
+_lib.lg_page_compact.argtypes = [_MP, _i32, _vp, _vp, _vp, _vp, _vp, _sz, _vp]
 _lib.lg_rope_frequencies.restype = ctypes.c_int
 _lib.lg_rope_frequencies.argtypes = [ctypes.POINTER(RopeParams), _vp, ctypes.POINTER(ctypes.c_float)]
 _lib.lg_rope_append.restype = ctypes.c_int
@@ -302,21 +302,24 @@ def lg_copy_bandwidth(src, dst, nbytes: int, stream=None):
 # ------------------------------------------------------------------------------------------------
 # The paged cache (include/lg_paged.h).
 # ------------------------------------------------------------------------------------------------
+# A decode step makes these calls for every layer, and the small ones take the GPU less time than the host: one
+# comparison a property, and no message before something is wrong.
 def _need(x, dtype, n, device, what):
-    """Refuses a tensor that is not dense, of this type, on this device and of at least n values."""
-    if x.dtype is not dtype or x.numel() < n or not x.is_contiguous() or x.get_device() != device:
-        raise LGError("%s: needs a contiguous %s tensor of %d values on device %d, got %s %s on %s" %
-                      (what, dtype, n, device, x.dtype, tuple(x.shape), x.device))
-    return x.data_ptr()
+    """The address of a tensor that is dense, of this type, on this device and of at least n values."""
+    if x.dtype is dtype and x.numel() >= n and x.is_contiguous() and x.get_device() == device:
+        return x.data_ptr()
+    raise LGError("%s: needs a contiguous %s tensor of %d values on device %d, got %s %s on %s" %
+                  (what, dtype, n, device, x.dtype, tuple(x.shape), x.device))
 
 
-def _on(device: int, layer=None):
-    """The paged calls run on the current device, which has to be the map's and the layer's."""
+def _on(device: int, stream, layer=None):
+    """The stream of a paged call, which runs on the current device: the map's and the layer's."""
     if layer is not None and layer.device != device:
         raise LGError("the layer's pages are on device %d, the page map on device %d" % (layer.device, device))
     if torch.cuda.current_device() != device:
         raise LGError("the page map is on device %d, the current device is %d" %
                       (device, torch.cuda.current_device()))
+    return _current_raw_stream(device) if stream is None else _stream(stream)
 
 
 def _bytes(workspace, device, what):
@@ -354,10 +357,11 @@ def paged_layer(k: torch.Tensor, v: torch.Tensor, n_q_heads: int) -> PagedLayer:
 
 
 def _layers(layers: Sequence[PagedLayer], device):
+    """The views side by side, as the host array that the C side reads during the call."""
     for l in layers:
         if l.device != device:
             raise LGError("a layer's pages are on device %d, the page map on device %d" % (l.device, device))
-    return (PagedLayer * len(layers))(*layers) if layers else None
+    return b"".join(layers) or None
 
 
 def lg_page_workspace(m: PageMap) -> int:
@@ -366,29 +370,29 @@ def lg_page_workspace(m: PageMap) -> int:
 
 def lg_page_reserve(m: PageMap, layers: Sequence[PagedLayer], q_start, t, base, workspace, stream=None):
     dev, B, i32 = m.device, m.batch, torch.int32
-    _on(dev)
+    stream = _on(dev, stream)
     ws, size = _bytes(workspace, dev, "workspace")
     _check(_lib.lg_page_reserve(ctypes.byref(m), len(layers), _layers(layers, dev),
                                 _need(q_start, i32, B + 1, dev, "q_start"), _need(t, i32, B, dev, "t"),
-                                _need(base, i32, B, dev, "base"), ws, size, _stream(stream)),
+                                _need(base, i32, B, dev, "base"), ws, size, stream),
            "lg_page_reserve")
 
 
 def lg_page_fork(m: PageMap, parent, workspace, stream=None):
-    _on(m.device)
+    stream = _on(m.device, stream)
     ws, size = _bytes(workspace, m.device, "workspace")
     _check(_lib.lg_page_fork(ctypes.byref(m), _need(parent, torch.int32, m.batch, m.device, "parent"),
-                             ws, size, _stream(stream)), "lg_page_fork")
+                             ws, size, stream), "lg_page_fork")
 
 
 def lg_page_compact(m: PageMap, layers: Sequence[PagedLayer], keep_idx, new_len, moved, workspace, stream=None):
     dev, B, i32 = m.device, m.batch, torch.int32
-    _on(dev)
+    stream = _on(dev, stream)
     ws, size = _bytes(workspace, dev, "workspace")
     _check(_lib.lg_page_compact(ctypes.byref(m), len(layers), _layers(layers, dev),
                                 _need(keep_idx, i32, B * m.max_pages * m.page_size, dev, "keep_idx"),
                                 _need(new_len, i32, B, dev, "new_len"), _need(moved, i32, B, dev, "moved"),
-                                ws, size, _stream(stream)), "lg_page_compact")
+                                ws, size, stream), "lg_page_compact")
 
 
 def lg_rope_frequencies(params: RopeParams):
@@ -402,17 +406,18 @@ def lg_rope_frequencies(params: RopeParams):
 
 def _rows(x, heads, D, dtype, device, what):
     """(pointer, row stride) of x [total][heads][D], whose rows may lie apart."""
-    if x.dtype is not dtype or x.dim() != 3 or x.shape[1] != heads or x.shape[2] != D or \
-            x.stride(2) != 1 or x.stride(1) != D or x.get_device() != device:
-        raise LGError("%s: needs a %s tensor [rows][%d][%d] on device %d with dense heads, got %s %s on %s" %
-                      (what, dtype, heads, D, device, x.dtype, tuple(x.shape), x.device))
-    return x.data_ptr(), (x.stride(0) if x.shape[0] > 1 else heads * D)
+    shape, stride = x.shape, x.stride()
+    if x.dtype is dtype and len(shape) == 3 and shape[1] == heads and shape[2] == D and stride[2] == 1 and \
+            (stride[1] == D or heads == 1) and x.get_device() == device:
+        return x.data_ptr(), (stride[0] if shape[0] > 1 else heads * D)
+    raise LGError("%s: needs a %s tensor [rows][%d][%d] on device %d with dense heads, got %s %s on %s" %
+                  (what, dtype, heads, D, device, x.dtype, tuple(shape), x.device))
 
 
 def lg_rope_append(layer: PagedLayer, m: PageMap, q, k, v, inv_freq, rot_dim: int, interleaved, scale: float,
                    q_out, q_start, base, stream=None):
     dev, D, dt, i32 = m.device, layer.head_dim, layer.torch_dtype, torch.int32
-    _on(dev, layer)
+    stream = _on(dev, stream, layer)
     total = q.shape[0]
     qp, qs = _rows(q, layer.n_q_heads, D, dt, dev, "q")
     kp = vp = None
@@ -427,7 +432,7 @@ def lg_rope_append(layer: PagedLayer, m: PageMap, q, k, v, inv_freq, rot_dim: in
                                int(bool(interleaved)), scale,
                                _need(q_out, dt, total * layer.n_q_heads * D, dev, "q_out"),
                                _need(q_start, i32, m.batch + 1, dev, "q_start"),
-                               _need(base, i32, m.batch, dev, "base"), total, _stream(stream)),
+                               _need(base, i32, m.batch, dev, "base"), total, stream),
            "lg_rope_append")
 
 
@@ -438,7 +443,7 @@ def lg_paged_attend_workspace(layer: PagedLayer, m: PageMap, total: int, max_chu
 def lg_paged_attend(layer: PagedLayer, m: PageMap, q, out, q_start, base, max_chunk: int, window: int,
                     n_sink: int, suffix_w, lse, suffix_mass, conf, workspace, stream=None):
     dev, B, dt, i32, f32 = m.device, m.batch, layer.torch_dtype, torch.int32, torch.float32
-    _on(dev, layer)
+    stream = _on(dev, stream, layer)
     total, n = q.shape[0], q.shape[0] * layer.n_q_heads
     ws, size = _bytes(workspace, dev, "workspace")
     _check(_lib.lg_paged_attend(
@@ -448,7 +453,7 @@ def lg_paged_attend(layer: PagedLayer, m: PageMap, q, out, q_start, base, max_ch
         None if suffix_w is None else _need(suffix_w, i32, B, dev, "suffix_w"),
         _need(lse, f32, n, dev, "lse"),
         None if suffix_mass is None else _need(suffix_mass, f32, n, dev, "suffix_mass"),
-        None if conf is None else _need(conf, f32, B, dev, "conf"), ws, size, _stream(stream)),
+        None if conf is None else _need(conf, f32, B, dev, "conf"), ws, size, stream),
         "lg_paged_attend")
 
 
