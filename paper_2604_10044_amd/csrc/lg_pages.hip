@@ -364,85 +364,97 @@ struct MoveArgs {
 };
 
 constexpr int kMoveThreads = 512;
-constexpr int kMoveUnroll = 4;
+constexpr int kMoveUnroll = 4;  // rows in flight per thread
 constexpr int kColBytes = 128;
 constexpr int kColLanes = kColBytes / 16;
 constexpr int kPassRows = kMoveThreads / kColLanes;
 constexpr int kRowsPerPass = kPassRows * kMoveUnroll;
+constexpr int kSegmentRows = 2048;  // rows whose places are looked up at once
 constexpr int kMoveWorkgroups = 1024;
+constexpr uint32_t kStays = 0xffffffffu;
 
-// A workgroup moves one 128-byte column of one head's K or V rows of one sequence, in passes of ascending
-// rows whose loads complete before their stores (as the contiguous compaction does: sources lie at or
-// above the rows they fill, so what a pass writes in place no later pass reads, and fresh pages are
-// nobody's source).
+// A workgroup moves one 128-byte column of one head's K or V rows of one sequence, in passes of ascending rows
+// whose loads complete before their stores (as the contiguous compaction does: sources lie at or above
+// the rows they fill, so what a pass writes in place no later pass reads, and fresh pages are nobody's
+// source). Where a row comes from and goes to takes two dependent loads (keep_idx, then the columns of both
+// ends), so a segment's rows look them up together and the passes find them in LDS, as slots of the pool (page x
+// page_size + row: below 2^32, since a slot has 128 bytes at least).
 struct Moves {
   u32x4_t x[kMoveUnroll];
-  int src[kMoveUnroll], dst[kMoveUnroll];  // rows of the pool for this head, -1: nothing to move
 };
 
-__device__ __forceinline__ void move_load(const MoveArgs& a, Moves& v, int r0, int nl, int b, int h,
+__device__ __forceinline__ size_t pool_row(const MapArgs& m, uint32_t slot, int Hkv, int h) {
+  return (((size_t)(slot >> m.shift) * Hkv + h) << m.shift) + (slot & ((1u << m.shift) - 1));
+}
+
+__device__ __forceinline__ void move_load(const MoveArgs& a, Moves& v, int r0, int n, int h, const uint32_t* src,
                                           const char* col) {
-  const MapArgs& m = a.map;
-  const int rsub = threadIdx.x / kColLanes, mask = (1 << m.shift) - 1;
-  int from[kMoveUnroll];
 #pragma unroll
   for (int u = 0; u < kMoveUnroll; ++u) {
-    const int r = r0 + u * kPassRows + rsub;
-    from[u] = r < nl ? a.keep_idx[(size_t)b * m.cap + r] : -1;
-  }
-#pragma unroll
-  for (int u = 0; u < kMoveUnroll; ++u) {
-    const int r = r0 + u * kPassRows + rsub;
-    v.src[u] = -1;
-    if (from[u] >= r && from[u] < m.cap) {
-      const int s = a.ws.table[(size_t)b * m.P + (from[u] >> m.shift)];
-      const int d = m.table[(size_t)b * m.P + (r >> m.shift)];
-      if (s >= 0 && is_page(m, d)) {
-        const int sp = s & ~kSharedMark;
-        if (sp != d || from[u] != r) v.src[u] = 0;
-        v.x[u] = v.src[u] == 0
-                     ? __builtin_nontemporal_load((const u32x4_t*)(
-                           col + ((((size_t)sp * a.Hkv + h) << m.shift) + (from[u] & mask)) * a.row_bytes))
-                     : u32x4_t{};
-        v.dst[u] = d;
-      }
-    }
+    const int r = r0 + u * kPassRows + (int)threadIdx.x / kColLanes;
+    const uint32_t s = r < n ? src[r] : kStays;
+    if (s != kStays)
+      v.x[u] = __builtin_nontemporal_load((const u32x4_t*)(col + pool_row(a.map, s, a.Hkv, h) * a.row_bytes));
   }
 }
 
-__device__ __forceinline__ void move_store(const MoveArgs& a, const Moves& v, int r0, int h, char* col) {
-  const MapArgs& m = a.map;
-  const int rsub = threadIdx.x / kColLanes, mask = (1 << m.shift) - 1;
+__device__ __forceinline__ void move_store(const MoveArgs& a, const Moves& v, int r0, int n, int h, const uint32_t* src,
+                                           const uint32_t* dst, char* col) {
 #pragma unroll
   for (int u = 0; u < kMoveUnroll; ++u) {
-    const int r = r0 + u * kPassRows + rsub;
-    if (v.src[u] == 0)
-      __builtin_nontemporal_store(
-          v.x[u], (u32x4_t*)(col + ((((size_t)v.dst[u] * a.Hkv + h) << m.shift) + (r & mask)) * a.row_bytes));
+    const int r = r0 + u * kPassRows + (int)threadIdx.x / kColLanes;
+    if (r < n && src[r] != kStays)
+      __builtin_nontemporal_store(v.x[u], (u32x4_t*)(col + pool_row(a.map, dst[r], a.Hkv, h) * a.row_bytes));
   }
 }
 
 __global__ __launch_bounds__(kMoveThreads) void move_rows(MoveArgs a) {
-  const int per = a.n_layers * a.Hkv * a.n_col;
+  __shared__ uint32_t src[kSegmentRows], dst[kSegmentRows];
+  const MapArgs& m = a.map;
+  const int per = a.n_layers * a.Hkv * a.n_col, mask = (1 << m.shift) - 1;
   const long long items = (long long)a.ws.count[0] * per;
+  int last = -1;  // the sequence whose places LDS holds, if all of them
   for (long long it = blockIdx.x; it < items; it += gridDim.x) {
     const int b = a.ws.list[it / per], x = (int)(it % per);
     const int l = x % a.n_layers, y = x / a.n_layers;
     const int c = y % a.n_col, h = y / a.n_col, half = a.n_col / 2;
     char* col = (char*)(c < half ? a.layer.k[l] : a.layer.v[l]) + (c % half) * kColBytes +
                 16 * (threadIdx.x % kColLanes);
-    const int nl = min(a.new_len[b], a.map.cap);
-    const int begin = a.ws.first[b] << a.map.shift;
-    Moves cur, nxt;
-    move_load(a, cur, begin, nl, b, h, col);
-    for (int r0 = begin; r0 < nl; r0 += kRowsPerPass) {
-      __syncthreads();  // every thread holds this pass's rows
-      const bool more = r0 + kRowsPerPass < nl;
-      if (more) move_load(a, nxt, r0 + kRowsPerPass, nl, b, h, col);
-      move_store(a, cur, r0, h, col);
-      if (more) cur = nxt;
+    const int nl = min(a.new_len[b], m.cap);
+    const int32_t* keep = a.keep_idx + (size_t)b * m.cap;
+    const int32_t *from = a.ws.table + (size_t)b * m.P, *to = m.table + (size_t)b * m.P;
+    const int begin = a.ws.first[b] << m.shift;
+    for (int g0 = begin; g0 < nl; g0 += kSegmentRows) {
+      const int n = min(nl - g0, kSegmentRows);
+      if (b != last) {
+        __syncthreads();  // the segment before is done
+        for (int i = threadIdx.x; i < n; i += kMoveThreads) {
+          const int r = g0 + i, k = keep[r];
+          uint32_t s = kStays, d = 0;
+          if (k >= r && k < m.cap) {
+            const int sp = from[k >> m.shift], dp = to[r >> m.shift];
+            if (sp >= 0 && is_page(m, dp)) {
+              s = ((uint32_t)(sp & ~kSharedMark) << m.shift) + (k & mask);
+              d = ((uint32_t)dp << m.shift) + (r & mask);
+              if (s == d) s = kStays;
+            }
+          }
+          src[i] = s;
+          dst[i] = d;
+        }
+        __syncthreads();
+      }
+      Moves cur, nxt;
+      move_load(a, cur, 0, n, h, src, col);
+      for (int r0 = 0; r0 < n; r0 += kRowsPerPass) {
+        __syncthreads();  // every thread holds this pass's rows
+        const bool more = r0 + kRowsPerPass < n;
+        if (more) move_load(a, nxt, r0 + kRowsPerPass, n, h, src, col);
+        move_store(a, cur, r0, n, h, src, dst, col);
+        if (more) cur = nxt;
+      }
     }
-    __syncthreads();
+    last = nl - begin <= kSegmentRows ? b : -1;
   }
 }
 
