@@ -203,26 +203,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
   const int tok = Rc / a.G, g = Rc - tok * a.G;
   const size_t qrow = (size_t)(job.first + tok) * a.Hq + job.h * a.G + g;
   const int slot_q = job.base + tok;
-  const int p_q = pos[slot_q];
-  const int sw = a.suffix_w != nullptr ? a.suffix_w[job.b] : 0;
-  // the row sees pos > win and, of these, counts pos > suf as its suffix
-  const int win = a.window > 0 ? (int)max((long long)p_q - a.window, (long long)INT32_MIN) : INT32_MIN;
-  const int suf = (int)max((long long)p_q - max(sw, 0), (long long)INT32_MIN);
-  // bounds over the wave's rows (tokens ascend with the row, positions with the token)
-  const int slot_lo = __builtin_amdgcn_readlane(slot_q, 0), slot_hi = __builtin_amdgcn_readlane(slot_q, 31);
-  const int win_hi = __builtin_amdgcn_readlane(win, 31);
-  const int suf_lo = __builtin_amdgcn_readlane(suf, 0), suf_hi = __builtin_amdgcn_readlane(suf, 31);
   const bool idle = wrow0 >= job.rows;  // KW = 1: a wave without rows only loads
-
-  // Q as the B operand: bf16: values 16 kk + 8 half ..; float32: values half D / 2 + 4 u ..
-  constexpr int NQ = F32 ? D / 8 : D / 16;
-  u32x4_t qf[NQ];
-  {
-    const char* src = (const char*)a.q + qrow * RB;
-#pragma unroll
-    for (int i = 0; i < NQ; ++i)
-      qf[i] = *(const u32x4_t*)(src + (F32 ? half * (RB / 2) + 16 * i : 32 * i + 16 * half));
-  }
 
   f32x16 O[ND];
 #pragma unroll
@@ -249,6 +230,27 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     load_lds4(table + (s >> m.shift), to);
     load_lds4(pos + s, to + 64);
   };
+  // What depends on the sequence alone is asked for together: the first tile's lookup, the queries, positions.
+  if (t_first < t_end) look(t_first, ring);
+  // Q as the B operand: bf16: values 16 kk + 8 half ..; float32: values half D / 2 + 4 u ..
+  constexpr int NQ = F32 ? D / 8 : D / 16;
+  u32x4_t qf[NQ];
+  {
+    const char* src = (const char*)a.q + qrow * RB;
+#pragma unroll
+    for (int i = 0; i < NQ; ++i)
+      qf[i] = *(const u32x4_t*)(src + (F32 ? half * (RB / 2) + 16 * i : 32 * i + 16 * half));
+  }
+
+  const int p_q = pos[slot_q];
+  const int sw = a.suffix_w != nullptr ? a.suffix_w[job.b] : 0;
+  // the row sees pos > win and, of these, counts pos > suf as its suffix
+  const int win = a.window > 0 ? (int)max((long long)p_q - a.window, (long long)INT32_MIN) : INT32_MIN;
+  const int suf = (int)max((long long)p_q - max(sw, 0), (long long)INT32_MIN);
+  // bounds over the wave's rows (tokens ascend with the row, positions with the token)
+  const int slot_lo = __builtin_amdgcn_readlane(slot_q, 0), slot_hi = __builtin_amdgcn_readlane(slot_q, 31);
+  const int win_hi = __builtin_amdgcn_readlane(win, 31);
+  const int suf_lo = __builtin_amdgcn_readlane(suf, 0), suf_hi = __builtin_amdgcn_readlane(suf, 31);
   // The position of the lane's slot, kHidden without a page.
   auto place = [&](const int32_t* at) __attribute__((always_inline)) { return is_page(m, at[lane]) ? at[64 + lane] : kHidden; };
   const int load0 = KW > 1 ? 0 : wave * C::kWaveLoad;  // the wave's first row of a tile
@@ -464,7 +466,6 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
   if (KW > 1 || tid == 0) *odd = 0;
   if constexpr (KW == 1) __syncthreads();
   if (t_first < t_end) {
-    look(t_first, ring);
     wait_loads<0>();
     const Groups gr = groups(t_first, ring);
     load_k(gr, my, 0);
@@ -814,56 +815,71 @@ __global__ __launch_bounds__(64 * KW) void paged_few(PagedAttendArgs a) {
   paged_body<T, D, KW, DV>(a, job, lds, (int32_t*)(lds + few_lds<T, D, KW, DV>() - 4 * KW));
 }
 
-// Joins the splits of a row: a wave per query row of a token. What it reads of the partials does not depend on the
-// sequence (rows of no sequence hold anything), so all its loads are on their way at once: a lane per
-// split for the statistics, a lane per D / 64 values for the outputs.
-constexpr int kJoinRows = kPagedThreads / 64;
+// Joins the splits of a row: D / 4 lanes a query row of a token, four values each. What it reads of the partials
+// does not depend on the sequence (rows of no sequence hold anything), so its first loads are on their way while
+// the sequence is found.
 constexpr int kMaxNs = 64;
-constexpr int kJoinAhead = 8;  // splits whose outputs are loaded together
+constexpr int kJoinAhead = 8;  // splits that are loaded together
+
+template <int D>
+constexpr int join_rows() { return kPagedThreads / (D / 4); }
 
 template <typename T, int D>
 __global__ __launch_bounds__(kPagedThreads) void paged_join(PagedAttendArgs a) {
-  constexpr int E = D / 64;
-  typedef float fE __attribute__((ext_vector_type(E)));
-  const long long row = (long long)blockIdx.x * kJoinRows + (threadIdx.x >> 6);
   const long long rows = (long long)a.total * a.Hq;
-  if (row >= rows) return;
-  const int r = (int)(row / a.Hq), lane = threadIdx.x & 63;
-  const f32x4 st = lane < a.ns ? *(const f32x4*)(a.pml + (lane * rows + row) * 4) : f32x4{-INFINITY, 0.f, 0.f, 0.f};
-  fE y[kJoinAhead];
+  const long long first = (long long)blockIdx.x * join_rows<D>();
+  const long long row = min(first + threadIdx.x / (D / 4), rows - 1);
+  const int d = threadIdx.x % (D / 4) * 4;
+  f32x4 st[kJoinAhead], y[kJoinAhead];
   auto load = [&](int s0) {
 #pragma unroll
-    for (int i = 0; i < kJoinAhead; ++i)
-      if (s0 + i < a.ns) y[i] = *(const fE*)(a.po + ((s0 + i) * rows + row) * D + lane * E);
+    for (int i = 0; i < kJoinAhead; ++i) {
+      const long long at = min(s0 + i, a.ns - 1) * rows + row;
+      st[i] = *(const f32x4*)(a.pml + at * 4);
+      y[i] = *(const f32x4*)(a.po + at * D + d);
+    }
   };
   load(0);
-  const int b = seq_of_row(a.q_start, a.map.B, r);
-  if (b >= a.map.B) return;
-  const Chunk c = chunk_of(a.q_start, b, a.total);
-  const int base = a.base[b];
-  if (r < c.first || r >= c.first + c.n || c.n > a.max_chunk || base < 0 || base > a.map.cap - c.n) return;
-  float M = st[0], L, SF;
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) M = fmaxf(M, __shfl_xor(M, o, 64));
-  const float f = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(st[0] - M);
-  L = f * st[1];
-  SF = f * st[2];
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    L += __shfl_xor(L, o, 64);
-    SF += __shfl_xor(SF, o, 64);
-  }
-  fE x = {};
+  // the sequences of the workgroup's first row, and from there on those that end before this row
+  const int r = (int)(row / a.Hq);
+  int b = seq_of_row(a.q_start, a.map.B, (int)(first / a.Hq));
+  while (b < a.map.B && a.q_start[b + 1] <= r) ++b;
+  const bool some = b < a.map.B;
+  const Chunk c = some ? chunk_of(a.q_start, b, a.total) : Chunk{0, 0};
+  const int base = some ? a.base[b] : -1;
+  float M = -INFINITY, L = 0.f, SF = 0.f;
+  f32x4 x = {};
   for (int s0 = 0; s0 < a.ns; s0 += kJoinAhead) {
     if (s0 > 0) load(s0);
+    float top = M;
 #pragma unroll
     for (int i = 0; i < kJoinAhead; ++i)
-      if (s0 + i < a.ns) x += __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), s0 + i)) * y[i];
+      if (s0 + i < a.ns) top = fmaxf(top, st[i][0]);
+    const float ms = top == -INFINITY ? 0.f : top, f0 = __builtin_amdgcn_exp2f(M - ms);
+    L *= f0;
+    SF *= f0;
+    x *= f0;
+#pragma unroll
+    for (int i = 0; i < kJoinAhead; ++i)
+      if (s0 + i < a.ns) {
+        const float f = __builtin_amdgcn_exp2f(st[i][0] - ms);
+        L += f * st[i][1];
+        SF += f * st[i][2];
+        x += f * y[i];
+      }
+    M = top;
   }
+  if (first + threadIdx.x / (D / 4) >= rows) return;
+  if (r < c.first || r >= c.first + c.n || c.n > a.max_chunk || base < 0 || base > a.map.cap - c.n) return;
   const float inv = 1.f / L;
 #pragma unroll
-  for (int e = 0; e < E; ++e) ((T*)a.out)[row * D + lane * E + e] = (T)(L == 0.f ? 0.f : x[e] * inv);
-  if (lane == 0) {
+  for (int e = 0; e < 4; ++e) x[e] = L == 0.f ? 0.f : x[e] * inv;
+  T* dst = (T*)a.out + row * D + d;
+  if constexpr (sizeof(T) == 4)
+    *(f32x4*)dst = x;
+  else
+    *(u32x2_t*)dst = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+  if (d == 0) {
     a.lse[row] = L == 0.f ? -INFINITY : kLn2 * (M + __builtin_amdgcn_logf(L));
     const float mass = L == 0.f ? 0.f : SF * inv;
     if (a.suffix != nullptr) a.suffix[row] = mass;
@@ -963,7 +979,7 @@ static void launch_typed(const PagedAttendArgs& a, const PagedPlan& p, dim3 grid
     hipLaunchKernelGGL((paged_few<T, D, KW, D / 2>), grid, dim3(64 * KW), 0, st, a);
   const long rows = (long)a.total * a.Hq;
   if (p.ns > 1)
-    hipLaunchKernelGGL((paged_join<T, D>), dim3((unsigned)((rows + kJoinRows - 1) / kJoinRows)), dim3(kPagedThreads), 0,
+    hipLaunchKernelGGL((paged_join<T, D>), dim3((unsigned)((rows + join_rows<D>() - 1) / join_rows<D>())), dim3(kPagedThreads), 0,
                        st, a);
 }
 
