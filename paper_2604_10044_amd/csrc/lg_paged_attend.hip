@@ -24,6 +24,7 @@
 // number and position. There a value that some row does not see could still reach it as 0 x inf = NaN
 // through the matrix product: when such a tile holds a value that is not finite, its product is
 // formed term by term for the rows that see it.
+#include <algorithm>
 #include <type_traits>
 
 #include "lg_paged_internal.h"
@@ -711,8 +712,9 @@ __device__ __forceinline__ void job_tiles(const PagedAttendArgs& a, Job& job, in
   }
   const int n = job.sink_tiles + tiles - job.tile0;
   job.split = split;
-  job.t_begin = (int)((long long)n * split / a.ns);
-  job.t_end = (int)((long long)n * (split + 1) / a.ns);
+  // n <= 2^25 + 2 tiles, at most 64 splits: below 2^32
+  job.t_begin = (int)((unsigned)n * (unsigned)split / (unsigned)a.ns);
+  job.t_end = (int)((unsigned)n * (unsigned)(split + 1) / (unsigned)a.ns);
 }
 
 // A sequence of at most 32 query rows: false if it has none, more, or is refused.
@@ -736,7 +738,7 @@ __device__ __forceinline__ bool few_job(const PagedAttendArgs& a, Job& job, int 
 // sequence are Hkv apart, so with 8 heads (the XCDs are dealt workgroups in turn) they share an L2. The
 // tiles of many rows come first, the last of a sequence (the longest) before the others.
 template <typename T, int D>
-__global__ __launch_bounds__(kPagedThreads, 2) void paged_attend(PagedAttendArgs a) {
+__global__ __launch_bounds__(kPagedThreads, (sizeof(T) == 4 && D == 128 ? 1 : 2)) void paged_attend(PagedAttendArgs a) {
   __shared__ __align__(512) char lds[paged_lds<T, D>()];
   int32_t* const flags = (int32_t*)(lds + paged_lds<T, D>() - 16);
   const int per = a.Hkv * a.ns;
@@ -899,23 +901,23 @@ struct PagedPlan {
 
 // Workgroups for the split of a launch without long chunks: one a CU.
 constexpr long kFewTarget = 256;
+// Slots of a split at most, whatever the number of workgroups: what one long sequence among many short ones
+// may hold up the launch by. Decode steps of 32 / 8 heads over 65536 slots of capacity, at 8192 / 16384 / 32768
+// slots a split / no such bound: 63 sequences of 1000 slots and one of 60000 182 / 219 / 335 / 571 us, 64 sequences
+// of 1000 slots 103 / 76 / 65.5 / 48.6 (the capacity is all the host knows).
+constexpr long kMaxSplitSlotsPaged = 32768;
 
-static PagedPlan paged_plan(const lg_paged_layer& l, const lg_page_map& m, long total, long max_chunk) {
+// reach: slots that a token may see, by the capacity and the window.
+static PagedPlan paged_plan(const lg_paged_layer& l, const lg_page_map& m, long total, long max_chunk, long reach) {
   const long G = l.n_q_heads / l.n_kv_heads;
   PagedPlan p;
   p.many_tiles = 0;
   p.halves = 1;
   p.few = max_chunk * G <= kWaveRows;
-  const long cap = (long)m.max_pages * m.page_size;
-  const long most = (cap + kMinSplitSlots - 1) / kMinSplitSlots;
   long ns;
   if (p.few) {
     const long units = (long)m.batch * l.n_kv_heads;
     ns = kFewTarget / units;  // more than one a CU would run in two rounds
-    if (l.head_dim == 128 && ns == 2) {
-      ns = 1;
-      p.halves = 2;
-    }
   } else {
     if (total * G > kWaveRows) {
       // a sequence of n rows has at most n / 128 + 1 tiles, and more than 32 rows
@@ -926,10 +928,19 @@ static PagedPlan paged_plan(const lg_paged_layer& l, const lg_page_map& m, long 
     const long units = (p.many_tiles + m.batch) * l.n_kv_heads;
     ns = (kPagedTarget + units - 1) / units;
   }
-  if (ns > most) ns = most;
-  if (ns > kMaxNs) ns = kMaxNs;
-  p.ns = (int)(ns < 1 ? 1 : ns);
+  ns = std::min({ns, (reach + kMinSplitSlots - 1) / kMinSplitSlots, (long)kMaxNs});
+  const long least = std::min(reach / kMaxSplitSlotsPaged, (long)kMaxNs);
+  if (p.few && ns == 2 && least < 2 && l.head_dim == 128) {
+    ns = 1;
+    p.halves = 2;
+  }
+  p.ns = (int)std::max({ns, least, 1l});
   return p;
+}
+
+static long whole_reach(const lg_page_map& m) { return (long)m.max_pages * m.page_size; }
+static long window_reach(const lg_page_map& m, long max_chunk, long window, long n_sink) {
+  return window > 0 ? std::min(whole_reach(m), window + n_sink + max_chunk) : whole_reach(m);
 }
 
 static size_t paged_need(const lg_paged_layer& l, const PagedPlan& p, long total) {
@@ -938,29 +949,31 @@ static size_t paged_need(const lg_paged_layer& l, const PagedPlan& p, long total
 
 // Workgroups of the launch (a grid holds fewer than 2^32 threads).
 long paged_attend_grid(const lg_paged_layer& l, const lg_page_map& m, int total, int max_chunk) {
-  const PagedPlan p = paged_plan(l, m, total, max_chunk);
+  const PagedPlan p = paged_plan(l, m, total, max_chunk, whole_reach(m));
   return (p.many_tiles + m.batch) * l.n_kv_heads * p.ns * p.halves;
 }
 
-size_t paged_attend_need(const lg_paged_layer& l, const lg_page_map& m, int total, int max_chunk) {
-  return paged_need(l, paged_plan(l, m, total, max_chunk), total);
+size_t paged_attend_need(const lg_paged_layer& l, const lg_page_map& m, int total, int max_chunk, int window,
+                         int n_sink) {
+  return paged_need(l, paged_plan(l, m, total, max_chunk, window_reach(m, max_chunk, window, n_sink)), total);
 }
 
-// The largest need of any total up to this one and any max_chunk up to this one: for a given number of
-// splits the need grows with total, and the number falls as total grows, so the ends of its steps count.
+// The largest need of any total up to this one and any max_chunk up to this one, with any window (a shorter reach
+// has no more splits). For a given number of splits the need grows with total, and the number falls as total
+// grows, so the ends of its steps count.
 size_t paged_attend_bytes(const lg_paged_layer& l, const lg_page_map& m, int total, int max_chunk) {
   size_t most = 16;
   for (int form = 0; form < 2; ++form) {
     const long chunk = form == 0 ? 1 : max_chunk;
     long t = total;
     while (t > 0) {
-      const PagedPlan p = paged_plan(l, m, t, chunk);
+      const PagedPlan p = paged_plan(l, m, t, chunk, whole_reach(m));
       const size_t need = paged_need(l, p, t);
       if (need > most) most = need;
       long lo = 0, hi = t;  // the largest smaller total with more splits
       while (hi - lo > 1) {
         const long mid = (lo + hi) / 2;
-        if (paged_plan(l, m, mid, chunk).ns > p.ns) lo = mid; else hi = mid;
+        if (paged_plan(l, m, mid, chunk, whole_reach(m)).ns > p.ns) lo = mid; else hi = mid;
       }
       t = lo;
     }
@@ -987,7 +1000,7 @@ hipError_t launch_paged_attend(const lg_paged_layer& l, const lg_page_map& m, co
                                const int32_t* q_start, const int32_t* base, int total, int max_chunk,
                                int window, int n_sink, const int32_t* suffix_w, float* lse, float* suffix,
                                float* conf, void* ws, hipStream_t st) {
-  const PagedPlan p = paged_plan(l, m, total, max_chunk);
+  const PagedPlan p = paged_plan(l, m, total, max_chunk, window_reach(m, max_chunk, window, n_sink));
   PagedAttendArgs a = {};
   a.q = q;
   a.k = l.k;

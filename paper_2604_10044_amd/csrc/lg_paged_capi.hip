@@ -18,7 +18,8 @@ hipError_t launch_rope(const lg_paged_layer& l, const lg_page_map& m, const void
                        const float* inv_freq, int rot, bool interleaved, float scale, void* q_out,
                        const int32_t* q_start, const int32_t* base, int total, hipStream_t st);
 size_t paged_attend_bytes(const lg_paged_layer& l, const lg_page_map& m, int total, int max_chunk);
-size_t paged_attend_need(const lg_paged_layer& l, const lg_page_map& m, int total, int max_chunk);
+size_t paged_attend_need(const lg_paged_layer& l, const lg_page_map& m, int total, int max_chunk, int window,
+                         int n_sink);
 long paged_attend_grid(const lg_paged_layer& l, const lg_page_map& m, int total, int max_chunk);
 hipError_t launch_paged_attend(const lg_paged_layer& l, const lg_page_map& m, const void* q, void* out,
                                const int32_t* q_start, const int32_t* base, int total, int max_chunk,
@@ -27,9 +28,8 @@ hipError_t launch_paged_attend(const lg_paged_layer& l, const lg_page_map& m, co
 
 static bool misaligned(const void* p) { return ((uintptr_t)p & 15u) != 0; }
 
-// A grid holds fewer than 2^32 threads; the launches here have at most 512 a workgroup, those that
-// grow with the step 256.
-constexpr long kMaxGrid = 1 << 23;
+// A grid holds fewer than 2^32 threads; the launches that grow with the step have at most 512 a workgroup.
+constexpr long kMaxGrid = (1 << 23) - 1;
 
 static lg_status check_map(const lg_page_map* m) {
   if (m == nullptr || !m->table || !m->pos || !m->len || !m->ref) return LG_ERR_NULL;
@@ -208,7 +208,7 @@ lg_status lg_paged_attend(const lg_paged_layer* layer, const lg_page_map* map, c
   if (suffix_w == nullptr && (suffix_mass != nullptr || conf != nullptr)) return LG_ERR_NULL;
   if (window < 0 || n_sink < 0) return LG_ERR_PARAM;
   if (misaligned(q) || misaligned(out)) return LG_ERR_ALIGN;
-  s = check_workspace(workspace, workspace_bytes, paged_attend_need(*layer, *map, total, max_chunk));
+  s = check_workspace(workspace, workspace_bytes, paged_attend_need(*layer, *map, total, max_chunk, window, n_sink));
   if (s != LG_OK) return s;
   return done(launch_paged_attend(*layer, *map, q, out, q_start, base, total, max_chunk, window, n_sink,
                                   suffix_w, lse, suffix_mass, conf, workspace, stream));

@@ -90,7 +90,7 @@ class Attend:
             see = self.see.get(b)
             page = np.where((page >= 0) & (page < len(k)), page, 0)
             pos = self.pos_h[b, :m]
-            pick = np.arange(n) if tokens is None else np.unique(np.clip(tokens, -n, n - 1) % max(n, 1))
+            pick = np.arange(n) if tokens is None or n == 0 else np.unique(np.clip(tokens, -n, n - 1) % max(n, 1))
             best = 0.0
             for h in range(self.hkv):
                 kk, vv = k[page, h, slots % ps], v[page, h, slots % ps]
@@ -163,6 +163,38 @@ def test_long(dtype, D, hq, hkv, ps, have, n, window, sinks):
     a = Attend(dtype, D, hq, hkv, ps, have, n, window=window, sinks=sinks, seed=7)
     a.call()
     a.check(tokens=np.array([0, 1, 17, 63, 64, -1]))
+
+
+@pytest.mark.parametrize("dtype,D,hq,hkv,batch", [
+    (BF, 128, 4, 4, 32),    # 128 pairs: two workgroups share a row's outputs
+    (BF, 128, 14, 2, 45),   # 90 pairs: the last group of 8 is short
+    (BF, 128, 8, 1, 70),    # 70: three splits
+    (F32, 128, 4, 2, 50),   # 100 pairs in float32
+    (BF, 64, 16, 4, 32),
+    (BF, 128, 8, 8, 40),    # 320: one workgroup each
+])
+def test_decode_batches(dtype, D, hq, hkv, batch):
+    """A token a sequence at batch sizes that take each launch of the decode step."""
+    have = [(37 * b) % 700 for b in range(batch)]
+    a = Attend(dtype, D, hq, hkv, 16, have, [1] * batch, seed=batch)
+    a.call()
+    a.check()
+    w = Attend(dtype, D, hq, hkv, 16, have, [1] * batch, window=100, sinks=5, seed=batch)
+    w.call()
+    w.check()
+
+
+def test_long_capacity():
+    """More slots of capacity than a split may have: the launch splits rows though it has workgroups enough, and
+    most splits are empty."""
+    a = Attend(BF, 64, 32, 32, 256, [3, 700, 40, 0, 90, 2000, 31, 64, 5], [1, 1, 2, 1, 0, 1, 1, 40, 1], seed=23)
+    more = 300 - a.P
+    a.table_h = np.concatenate([a.table_h, np.full((9, more), -1)], 1)
+    a.pos_h = np.concatenate([a.pos_h, np.full((9, more * 256), -1)], 1)
+    assert 300 * 256 > 2 * 32768
+    a.alloc()
+    a.call()
+    a.check(tokens=np.array([0, 1, 39]))
 
 
 def test_long_prompt():
