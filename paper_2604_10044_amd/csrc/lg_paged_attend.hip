@@ -12,18 +12,34 @@
 // with lane ^ 32, and the rounded P is the B operand of the second product as it lies in the registers:
 // V^T is read in the same order of keys. Scores are in units of log 2 (exp2).
 //
-// Two shapes of workgroup in one launch (template KW, waves along the keys):
-//   KW = 1  sequences with more than 32 query rows: 128 rows, four waves of 32, which share every tile.
-//   KW = 4  the others (a decode step: G rows): the four waves take every fourth tile of the sequence, each
-//           with LDS of its own and no barrier, and their (m, l, O) are joined at the end.
+// Workgroups (template KW, waves along the keys):
+//   KW = 1  sequences with more than 32 query rows: 128 rows, four waves of 32, which share every tile of 64
+//           slots (32 in float32), two buffers, one barrier a tile, two workgroups a CU. A row's share of K and
+//           V then comes from LDS four times as often as from the L2.
+//   KW > 1  the others (a decode step: G rows): the waves take every KW-th tile of 32 slots, each with LDS of its
+//           own and no barrier, and their (m, l, O) are joined at the end. paged_few is the launch for steps that
+//           have no others, 8 waves a workgroup; beside long chunks it is four (paged_attend).
 // When these workgroups are fewer than the CUs hold, the slots of a row are split over several and a second
-// launch joins them.
+// launch joins them (paged_plan).
 //
 // A tile whose slots every row of the wave sees needs no comparison. In the others (the end of the
-// causal triangle, the edges of the window and of the suffix) visibility is decided slot by slot from its
-// number and position. There a value that some row does not see could still reach it as 0 x inf = NaN
-// through the matrix product: when such a tile holds a value that is not finite, its product is
-// formed term by term for the rows that see it.
+// causal triangle, the edges of the window) visibility is decided slot by slot. There a value that some
+// row does not see could still reach it as 0 x inf = NaN through the matrix product: such a tile's values that
+// are not finite count as 0 in it, and reach the rows that see them in a pass behind the loop.
+//
+// What bounds it, measured on MI355X (a copy reaches 5.2 TB/s, a bfloat16 matrix product of 8192^3 1100
+// TFLOP/s): a decode step of 32 sequences of 28 / 4 heads and 1280 to 2047 slots, 112 MB, 23.2 us in a graph, 4.8
+// TB/s: the memory. 4096 tokens of 32 / 8 heads behind 4096, 412 GFLOP, 433 to 474 us by card, 870 to 950
+// TFLOP/s: of a wave's time a third is matrix instructions and as much the exponentials with their maxima, sums
+// and roundings, which the other wave of its SIMD covers in part; the rest is issuing loads and scalar code.
+// float32 runs at 107 of the 154 TFLOP/s of a float32 product. 128 tokens each of four sequences with a window
+// of 2048 beside 12 decoding ones, 147 MB: 55 to 60 us, the length of a workgroup's chain of 17 tiles and the
+// launch that joins two splits.
+//
+// Tried and left: 8 waves sharing the tiles of 256 rows, one workgroup a CU (422 against 440 us for the 4096
+// tokens, but 85 against 54 for the mixed step and 177 against 163 for chunks of 512 at head_dim 64); tiles of 32
+// slots four deep with counted waits (510 us); the scores of the next tile beside this one's exponentials (539
+// us: registers spill).
 #include <algorithm>
 #include <type_traits>
 
@@ -43,7 +59,8 @@ typedef short i16x4 __attribute__((ext_vector_type(4)));
 constexpr int kWaveRows = 32;
 constexpr int kManyRows = 128;   // rows of a KW = 1 workgroup
 constexpr int kPagedThreads = 256;
-// Workgroups a launch aims for by splitting slots: two a CU.
+// Workgroups a launch with long chunks aims for by splitting slots: two a CU. The mixed step above at 256 / 512 /
+// 1024: 72 / 58.6 / 61 us, 256 tokens behind 16128 slots 108 / 101 / 115.
 constexpr long kPagedTarget = 512;
 constexpr int kMinSplitSlots = 256;  // slots of a split at least (by capacity)
 constexpr float kSlack = 8.f;  // see paged_body
@@ -797,6 +814,8 @@ __global__ __launch_bounds__(kPagedThreads, (sizeof(T) == 4 && D == 128 ? 1 : 2)
 // a sequence's slots are swept by as many loads as the memory needs on their way with one workgroup a CU.
 // DV < D: two workgroups a KV head, each with all of K and half of V, in place of a split of the slots: no
 // second launch to join them, and K comes to the second from the L2 of their XCD (they are 8 workgroups apart).
+// For the 128 pairs of the decode step above 26.4 us a call, 34.4 with four-wave workgroups, four splits and the
+// launch that joins them (24 and 8 us).
 // Grid: (Hkv, ns, B) flattened into units; with two halves, groups of 8 units' first halves, then their second.
 template <typename T, int D, int KW, int DV>
 __global__ __launch_bounds__(64 * KW) void paged_few(PagedAttendArgs a) {
