@@ -150,6 +150,15 @@ def test_fork_permutes():
     p.fork([0, 1, 2, 3, 4, 5])
 
 
+@pytest.mark.parametrize("P, lengths", [(64, [1024, 1023, 1025, 16384, 0]), (300, [76800, 65537, 65536, 1, 16640])])
+def test_fork_of_long_sequences(P, lengths):
+    """Rows that several workgroups copy, and more of them than the largest grid takes at once."""
+    p = Pool(5, P, 256, sum((n + 255) // 256 for n in lengths) + 1, L=1, Hkv=1, seed=8)
+    p.reserve(lengths, [n - 1 for n in lengths])
+    p.fork([3, 0, 2, 1, 0])
+    p.fork([1, 2, 0, -1, 3])
+
+
 def test_compact_in_place_and_shared():
     p = Pool(6, 8, 16, 70, L=2, Hkv=2, D=128, seed=6)
     p.reserve([128, 100, 77, 16, 5, 0], [127, 99, 76, 15, 4, 0])
