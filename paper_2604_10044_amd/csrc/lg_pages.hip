@@ -105,6 +105,10 @@ struct ReserveArgs {
   int32_t* base;
 };
 
+// Pages a sequence needs = ceil((len + n) / ps) - ceil(len / ps), and one more where its last page holds live
+// slots that others share. A few integers a sequence: the chain of dependent reads (len, table, ref, then the
+// scan of ref, then table) bounds it, not their bytes, so everything is one launch of one workgroup. Measured:
+// 5.9 us for 32 sequences of one token; a scan of 4096 pages is one round.
 __global__ __launch_bounds__(kMapThreads) void reserve_map(ReserveArgs a) {
   __shared__ int red[kMapWaves];
   __shared__ int copies;
@@ -182,7 +186,10 @@ struct CopyArgs {
 constexpr int kCopyThreads = 256;
 constexpr int kCopyWorkgroups = 1024;
 
-// The live rows of replaced last pages: an item is one layer's K or V of one head, contiguous rows.
+// The live rows of replaced last pages: an item is one layer's K or V of one head, contiguous rows, at most
+// page_size * row_bytes = 128 KB, that one workgroup copies in 16-byte pieces. How many there are is known on
+// the device only, so the grid is fixed and walks the items. Measured: 2.0 us with nothing to copy, 7.4 us for
+// eight forks of one prompt over 32 layers.
 __global__ __launch_bounds__(kCopyThreads) void copy_rows(CopyArgs a) {
   const int copies = a.ws.count[0];
   const int per = 2 * a.n_layers * a.Hkv;
@@ -290,6 +297,9 @@ __device__ __forceinline__ int rows_in_place(const int32_t* keep, int n) {
   return lo;
 }
 
+// Which columns change (from the first row that moves), which of those are shared and need a page, and the
+// references given back. Like reserve_map a chain of dependent reads: 5.2 us for one flagged sequence of
+// 32, 13.3 us for eight long ones that share their pages.
 __global__ __launch_bounds__(kMapThreads) void compact_map(CompactMapArgs a) {
   __shared__ int red[kMapWaves];
   __shared__ int moves;
@@ -389,6 +399,7 @@ constexpr uint32_t kStays = 0xffffffffu;
 // source). Where a row comes from and goes to takes two dependent loads (keep_idx, then the columns of both
 // ends), so a segment's rows look them up together and the passes find them in LDS, as slots of the pool (page x
 // page_size + row: below 2^32, since a slot has 128 bytes at least).
+// Memory bounds it: 3.0 GB in 534 us, 5.6 TB/s, where a copy of 1 GiB runs at 5.2.
 struct Moves {
   u32x4_t x[kMoveUnroll];
 };
