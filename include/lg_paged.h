@@ -28,8 +28,8 @@
  *
  * The map. `table[b][c]` is the page of slots [c page_size, (c + 1) page_size) of sequence b, or -1.
  * `ref[p]` counts the table entries that name page p: 0 is a free page. Live slots 0..len[b]-1 hold
- * strictly increasing positions, as in lg.h; the columns below ceil(len[b] / page_size) name pages
- * and the others are -1. An empty map is table = -1, len = 0, ref = 0. All calls here keep this, and
+ * strictly increasing positions, as in lg.h, below 2^31 - 1; the columns below
+ * ceil(len[b] / page_size) name pages and the others are -1. An empty map is table = -1, len = 0, ref = 0. All calls here keep this, and
  * ask for it: other values (a page number outside the pool, say) give unspecified results for the
  * sequences that hold them, without any access outside the buffers. A caller may hold pages back
  * by counting them once more in ref. Pages are taken in ascending order of their number, for the
@@ -80,7 +80,7 @@ size_t lg_page_workspace(const lg_page_map* map);
  * A sequence is refused when pages run out (see above) or n exceeds its columns: base[b] = -1, and
  * the calls that take base leave its rows alone. With n = 0, base[b] = len[b].
  *   layers       host array of n_layers views (0: the map alone; then the caller copies rows of pages).
- *                All have the same sizes and type (LG_ERR_SHAPE).
+ *                All have the same sizes and type (LG_ERR_SHAPE), and no pages in common.
  *   q_start      [batch + 1] int32, ascending.
  *   t            [batch] int32, newest position of each sequence after the step.
  *   base         [batch] int32 output. */
@@ -145,7 +145,8 @@ lg_status lg_rope_frequencies(const lg_rope_params* p, float* inv_freq, float* s
  *   q, k, v      row r, head h at x + r * stride + h * head_dim, strides in elements (>= heads *
  *                head_dim: LG_ERR_SHAPE); e.g. parts of one projection's rows. k and v may both be NULL
  *                (queries only). Arrays and rows are 16-byte aligned (LG_ERR_ALIGN).
- *   q_out        [total][n_q_heads][head_dim]; may be q itself when that is dense.
+ *   q_out        [total][n_q_heads][head_dim]; may be q itself when that is dense (LG_ERR_PARAM when it
+ *                is not), and overlaps none of q, k, v in any other way.
  *   inv_freq     [rot_dim / 2] float32 device array; may be NULL with rot_dim 0 (append alone).
  *   rot_dim      even, 0 <= rot_dim <= head_dim (LG_ERR_PARAM).
  *   total        rows of q, k and v; 0 enqueues nothing. */
@@ -173,7 +174,8 @@ size_t lg_paged_attend_workspace(const lg_paged_layer* layer, const lg_page_map*
  * (its pages are missing) gets out = 0, lse = -inf, suffix_mass = 0. A refused sequence
  * (base[b] < 0) with tokens has conf[b] = NaN, which lg_detect_loop reads as "attend_error"; its
  * rows, and rows from q_start[batch] on, are left as they are.
- *   q, out       [total][n_q_heads][head_dim] dtype, 16-byte aligned; out may not overlap q.
+ *   q, out       [total][n_q_heads][head_dim] dtype, 16-byte aligned; out may not overlap q (LG_ERR_PARAM
+ *                for out = q).
  *   max_chunk    the largest number of tokens of a sequence; one that brings more is treated as
  *                refused. total, max_chunk: >= 0; 0 total enqueues nothing.
  *   window, n_sink  >= 0 (LG_ERR_PARAM).
@@ -182,7 +184,8 @@ size_t lg_paged_attend_workspace(const lg_paged_layer* layer, const lg_page_map*
  *   lse, suffix_mass [total][n_q_heads] float32; suffix_mass may be NULL; conf [batch] or NULL.
  *   workspace    16-byte aligned (LG_ERR_ALIGN, LG_ERR_WORKSPACE).
  * bfloat16 layers multiply alpha as bfloat16 with V (one rounding of each weight before the float32
- * sum); lse and suffix_mass are sums of the float32 weights. */
+ * sum); lse and suffix_mass are sums of the float32 weights. An infinity in v whose weight is so small that
+ * it rounds to 0 gives a token that sees it that infinity or NaN. */
 lg_status lg_paged_attend(const lg_paged_layer* layer, const lg_page_map* map, const void* q,
                           void* out, const int32_t* q_start, const int32_t* base, int32_t total,
                           int32_t max_chunk, int32_t window, int32_t n_sink,

@@ -183,6 +183,7 @@ lg_status lg_rope_append(const lg_paged_layer* layer, const lg_page_map* map, co
   if (q_stride < wq || (k != nullptr && (k_stride < wk || v_stride < wk))) return LG_ERR_SHAPE;
   if (q_stride > (int64_t)1 << 40 || k_stride > (int64_t)1 << 40 || v_stride > (int64_t)1 << 40) return LG_ERR_SHAPE;
   if (total < 0 || total > kMaxGrid) return LG_ERR_SHAPE;
+  if (q_out == q && total > 1 && q_stride != wq) return LG_ERR_PARAM;  // rows would be read after others' are written
   const int64_t e = layer->dtype == LG_BF16 ? 2 : 4;
   if (misaligned(q) || misaligned(q_out) || misaligned(k) || misaligned(v)) return LG_ERR_ALIGN;
   if (q_stride * e % 16 != 0 || (k != nullptr && (k_stride * e % 16 != 0 || v_stride * e % 16 != 0)))
@@ -206,7 +207,7 @@ lg_status lg_paged_attend(const lg_paged_layer* layer, const lg_page_map* map, c
   if (s != LG_OK || total == 0) return s;
   if (!q || !out || !q_start || !base || !lse) return LG_ERR_NULL;
   if (suffix_w == nullptr && (suffix_mass != nullptr || conf != nullptr)) return LG_ERR_NULL;
-  if (window < 0 || n_sink < 0) return LG_ERR_PARAM;
+  if (window < 0 || n_sink < 0 || out == q) return LG_ERR_PARAM;
   if (misaligned(q) || misaligned(out)) return LG_ERR_ALIGN;
   s = check_workspace(workspace, workspace_bytes, paged_attend_need(*layer, *map, total, max_chunk, window, n_sink));
   if (s != LG_OK) return s;

@@ -262,3 +262,12 @@ def test_binding_refuses_host_tensors():
         lg.paged_layer(torch.zeros(16, 2, 16, 64), torch.zeros(16, 2, 16, 64), 4)
     with pytest.raises(lg.LGError):
         lg.paged_layer(torch.zeros(16, 2, 16, 64, dtype=torch.float16), torch.zeros(16, 2, 16, 64, dtype=torch.float16), 4)
+
+
+def test_calls_in_place():
+    """Queries may be rotated in place when their rows are dense; attention has no form in place."""
+    lg = _lg()
+    m, l = _map(lg), _layer(lg)
+    assert _rope(lg, l, m, out=0x10, qs=1032) == 4
+    assert _rope(lg, l, m, out=0x10, qs=1032, total=0) == 0
+    assert _attend(lg, l, m, out=0x10) == 4
