@@ -268,6 +268,9 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
   // bounds over the wave's rows (tokens ascend with the row, positions with the token)
   const int slot_lo = __builtin_amdgcn_readlane(slot_q, 0), slot_hi = __builtin_amdgcn_readlane(slot_q, 31);
   const int win_hi = __builtin_amdgcn_readlane(win, 31);
+  // and over the workgroup's (KW = 1)
+  const int slot_lo_all = job.base + job.row0 / a.G;
+  const int win_hi_all = KW == 1 && a.window > 0 ? (int)max((long long)pos[last_slot] - a.window, (long long)INT32_MIN) : INT32_MIN;
   const int suf_lo = __builtin_amdgcn_readlane(suf, 0), suf_hi = __builtin_amdgcn_readlane(suf, 31);
   // The position of the lane's slot, kHidden without a page.
   auto place = [&](const int32_t* at) __attribute__((always_inline)) { return is_page(m, at[lane]) ? at[64 + lane] : kHidden; };
@@ -358,11 +361,10 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
   // at a time, as they lie in the accumulators' rows.
   int s0, tp;
   int32_t* at;
-  bool masked;
-  auto is_masked = [&]() __attribute__((always_inline)) {
+  // for rows whose first one is at slot lo and whose last one sees positions above hi
+  auto is_masked = [&](int lo, int hi) __attribute__((always_inline)) {
     const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
-    return __ballot(tp == kHidden) != 0 || s0 + NK - 1 > slot_lo ||
-           (a.window > 0 && p_first <= win_hi && p_last >= a.n_sink);
+    return __ballot(tp == kHidden) != 0 || s0 + NK - 1 > lo || (a.window > 0 && p_first <= hi && p_last >= a.n_sink);
   };
   auto four = [&](const int32_t* x, int nb, int i) __attribute__((always_inline)) {
     return *(const i32x4*)(x + 32 * nb + 8 * i + 4 * half);
@@ -420,8 +422,9 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     }
     return (s4[0] + s4[1]) + (s4[2] + s4[3]);
   };
-  // Puts 0 in the place of what is not finite in V of a tile (in LDS), and says so in *odd. With KW = 1 other waves
-  // may read the tile meanwhile: they find a value or its 0, and the pass behind the loop adds the value.
+  // Puts 0 in the place of what is not finite in V of a tile (in LDS), and says so in *odd. With KW = 1 the waves
+  // share the tile, so each that reads it does this first when any of them has to, all with the same result:
+  // what a wave then reads does not depend on the others' pace.
   auto make_finite = [&](char* v) __attribute__((always_inline)) {
     for (int i = lane; i < C::kTileV / 16; i += 64) {
       u32x4_t x = *(const u32x4_t*)(v + 16 * i);
@@ -506,13 +509,14 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
         scores(from, here + kBlock, S1);
         schedule_scores();
       }
-      masked = is_masked();
       const int how = suffix_of();
-      if (masked) {
-        set_bounds();
+      if (is_masked(slot_lo_all, win_hi_all)) {
         make_finite(const_cast<char*>(from) + here + C::kTile);
-        mask(S, 0);
-        if constexpr (NB > 1) mask(S1, 1);
+        if (is_masked(slot_lo, win_hi)) {
+          set_bounds();
+          mask(S, 0);
+          if constexpr (NB > 1) mask(S1, 1);
+        }
       }
       raise_max(NB > 1 ? fmaxf(top(S), top(S1)) : top(S));
       // Without a branch up to the sums: the second block's exponentials beside the first one's product.
@@ -544,7 +548,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
                              char* __restrict__ to, int32_t* __restrict__ ring_to) __attribute__((always_inline)) {
       if (more) load_k(gr, to, 0);
       look(t + 2 * KW, ring_to);
-      masked = is_masked();
+      const bool masked = is_masked(slot_lo, win_hi);
       const int how = suffix_of();
       if (masked) {
         set_bounds();

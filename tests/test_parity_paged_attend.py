@@ -282,6 +282,23 @@ def test_infinite_values_are_seen(dtype):
     assert np.isfinite(out[0]).all() and np.isfinite(np.delete(out[1], [3, 4], 1)).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_infinite_value_of_a_vanishing_weight(dtype):
+    """Waves that see a tile whole and waves that do not share it: a slot whose weight rounds to 0 and whose V is
+    infinite gives every token that sees it that infinity, whichever wave comes to the tile first."""
+    a = Attend(dtype, 64, 1, 1, 16, [0], [128], seed=14, holes=False)
+    a.q.fill_(1.0)
+    a.k.zero_()
+    p = int(a.table_h[0, 0])
+    a.k[p, 0, 10] = -1000.0  # a score of -8000
+    a.v[p, 0, 10, 3] = float("inf")
+    for _ in range(8):
+        a.call()
+        out = a.results()[0][:128, 0]
+        assert np.isfinite(out[:10]).all() and (out[10:, 3] == np.inf).all()
+        assert np.isfinite(np.delete(out, 3, 1)).all()
+
+
 def test_large_scores():
     """Scores of several hundred: weights of the far ones are 0, the lse is the largest score."""
     a = Attend(BF, 128, 4, 2, 16, [300, 20], [3, 40], seed=13, gain=60.0)
