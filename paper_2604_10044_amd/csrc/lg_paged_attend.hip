@@ -197,12 +197,59 @@ struct Job {
   int tile0;        // first tile of the rest
   int t_begin, t_end;  // this split's share of the sink_tiles + rest tiles
   int split;
+  int end;  // slots that any of its rows may see lie below
   int d0;  // first of the DV values of V
 };
 
+// This split's share of a workgroup's tiles: those for the first tokens, and those from tile0 to the last.
+__device__ __forceinline__ void share_tiles(const PagedAttendArgs& a, Job& job, int nk, int end, int tile0) {
+  job.tile0 = tile0;
+  job.sink_tiles = a.window > 0 ? min((min(a.n_sink, end) + nk - 1) / nk, tile0) : 0;
+  const int n = job.sink_tiles + (end + nk - 1) / nk - tile0;
+  // n <= 2^25 + 2 tiles, at most 64 splits: below 2^32
+  job.t_begin = (int)((unsigned)n * (unsigned)job.split / (unsigned)a.ns);
+  job.t_end = (int)((unsigned)n * (unsigned)(job.split + 1) / (unsigned)a.ns);
+}
+
+// The slots that the workgroup's rows may see, in tiles. A window's first slot is at least (slot - window + 1):
+// positions ascend by at least one a slot; slots below n_sink likewise hold the positions below n_sink.
+// Where the guard has pruned, the window holds fewer slots: skip_hidden.
+template <int NK>
+__device__ __forceinline__ void job_tiles(const PagedAttendArgs& a, Job& job, int rows_of_wg, int split) {
+  const int tok_lo = job.row0 / a.G;
+  const int tok_hi = (min(job.row0 + rows_of_wg, job.rows) - 1) / a.G;
+  const long long begin = a.window > 0 ? (long long)job.base + tok_lo - a.window + 1 : 0;
+  job.split = split;
+  job.end = min(job.base + tok_hi + 1, a.map.cap);
+  share_tiles(a, job, NK, job.end, begin > 0 ? (int)(begin / NK) : 0);
+}
+
+// Tiles behind the first tokens' that no row sees, by the window of the workgroup's first one: the first tile whose last
+// slot it sees, found by search, 64 probes a round. True if the share has changed. Without holes one read that the
+// first tile's lookup overlaps (59.6 us for the mixed step above, 60.2 without the search). 32 sequences of 8192 slots
+// that decode with a window of 4096 over a history thinned out four to one: 58 us, 100 without.
+template <int NK>
+__device__ __forceinline__ bool skip_hidden(const PagedAttendArgs& a, Job& job, const int32_t* pos) {
+  if (job.tile0 == 0) return false;  // no window, or all of the cache within it
+  const int slot = job.base + job.row0 / a.G, lane = threadIdx.x & 63;
+  const int w = (int)max((long long)pos[slot] - a.window, (long long)INT32_MIN);
+  int lo = job.tile0, hi = slot / NK;  // the tile of the token's own slot is seen
+  if (lo >= hi || pos[lo * NK + NK - 1] > w) return false;
+  while (lo < hi) {
+    const int step = (hi - lo + 63) >> 6;
+    const long long first = (long long)lo + (long long)lane * step;
+    const int at = (int)min(first + step - 1, (long long)hi - 1);
+    const int cnt = __popcll(__ballot(first < hi && pos[at * NK + NK - 1] <= w));
+    lo = (int)min((long long)lo + (long long)cnt * step, (long long)hi);
+    hi = step == 1 ? lo : (int)min((long long)lo + step - 1, (long long)hi);
+  }
+  share_tiles(a, job, NK, job.end, lo);
+  return true;
+}
+
 // flags: in LDS, one a team (see make_finite).
 template <typename T, int D, int KW, int DV>
-__device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& job, char* lds, int32_t* flags) {
+__device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, char* lds, int32_t* flags) {
   using C = Team<T, D, KW, DV>;
   constexpr bool F32 = C::kF32;
   constexpr int NK = C::kKeys, NB = NK / 32, ND = DV / 32, RB = C::kRowBytes, RBV = C::kRowBytesV;
@@ -230,8 +277,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
     for (int i = 0; i < 16; ++i) O[d][i] = 0.f;
   float mx = -INFINITY, l = 0.f, sfx = 0.f;  // l and sfx: the lane's half of the keys
 
-  const int t_end = job.t_end;
-  const int t_first = KW > 1 ? job.t_begin + wave : job.t_begin;
+  int t_end = job.t_end, t_first = KW > 1 ? job.t_begin + wave : job.t_begin;
   const int last_slot =  // the last one that any row of the workgroup sees
       job.base + (min(job.row0 + (KW > 1 ? kWaveRows : kManyRows), job.rows) - 1) / a.G;
   auto slot_of = [&](int t) __attribute__((always_inline)) { return (t < job.sink_tiles ? t : t - job.sink_tiles + job.tile0) * NK; };
@@ -261,6 +307,12 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
   }
 
   const int p_q = pos[slot_q];
+  if (skip_hidden<NK>(a, job, pos)) {
+    t_end = job.t_end;
+    t_first = KW > 1 ? job.t_begin + wave : job.t_begin;
+    wait_loads<0>();  // the first lookup has landed
+    if (t_first < t_end) look(t_first, ring);
+  }
   const int sw = a.suffix_w != nullptr ? a.suffix_w[job.b] : 0;
   // the row sees pos > win and, of these, counts pos > suf as its suffix
   const int win = a.window > 0 ? (int)max((long long)p_q - a.window, (long long)INT32_MIN) : INT32_MIN;
@@ -713,29 +765,6 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, const Job& 
       if (a.conf != nullptr && tk == job.rows / a.G - 1) raise_conf(a.conf + job.b, mass);
     }
   }
-}
-
-// The slots that the workgroup's rows may see, in tiles, and this split's share of them. A window's first
-// slot is at least (slot - window + 1): positions ascend by at least one a slot; slots below n_sink
-// likewise hold the positions below n_sink. Holes make the true range shorter: compared slot by slot.
-template <int NK>
-__device__ __forceinline__ void job_tiles(const PagedAttendArgs& a, Job& job, int rows_of_wg, int split) {
-  const int tok_lo = job.row0 / a.G;
-  const int tok_hi = (min(job.row0 + rows_of_wg, job.rows) - 1) / a.G;
-  const int end = min(job.base + tok_hi + 1, a.map.cap);
-  const int tiles = (end + NK - 1) / NK;
-  job.sink_tiles = 0;
-  job.tile0 = 0;
-  if (a.window > 0) {
-    const long long begin = (long long)job.base + tok_lo - a.window + 1;
-    job.tile0 = begin > 0 ? (int)(begin / NK) : 0;
-    job.sink_tiles = min((min(a.n_sink, end) + NK - 1) / NK, job.tile0);
-  }
-  const int n = job.sink_tiles + tiles - job.tile0;
-  job.split = split;
-  // n <= 2^25 + 2 tiles, at most 64 splits: below 2^32
-  job.t_begin = (int)((unsigned)n * (unsigned)split / (unsigned)a.ns);
-  job.t_end = (int)((unsigned)n * (unsigned)(split + 1) / (unsigned)a.ns);
 }
 
 // A sequence of at most 32 query rows: false if it has none, more, or is refused.

@@ -282,6 +282,20 @@ def test_infinite_values_are_seen(dtype):
     assert np.isfinite(out[0]).all() and np.isfinite(np.delete(out[1], [3, 4], 1)).all()
 
 
+@pytest.mark.parametrize("dtype, D, hq, hkv", [(BF, 128, 8, 2), (BF, 64, 6, 6), (F32, 128, 4, 1), (F32, 64, 4, 4)])
+@pytest.mark.parametrize("chunk", [1, 3, 70])
+@pytest.mark.parametrize("window, sinks", [(100, 4), (2500, 40), (9000, 0), (30000, 600)])
+def test_windows_over_pruned_history(dtype, D, hq, hkv, chunk, window, sinks):
+    """Histories thinned out eight to one, and a few slots behind one long gap: a window holds far fewer slots
+    than positions."""
+    a = Attend(dtype, D, hq, hkv, 32, [3200, 1500, 40], [1, chunk, chunk], window=window, sinks=sinks, seed=window + chunk)
+    a.pos_h = np.cumsum(np.where(np.arange(a.pos_h.shape[1]) < 30, 1, a.r.randint(1, 16, a.pos_h.shape)), 1) - 1
+    a.pos_h[1, 1450:] += 20000
+    a.alloc()
+    a.call()
+    a.check()
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_infinite_value_of_a_vanishing_weight(dtype):
     """Waves that see a tile whole and waves that do not share it: a slot whose weight rounds to 0 and whose V is
