@@ -62,7 +62,11 @@ constexpr int kPagedThreads = 256;
 // Workgroups a launch with long chunks aims for by splitting slots: two a CU. The mixed step above at 256 / 512 /
 // 1024: 72 / 58.6 / 61 us, 256 tokens behind 16128 slots 108 / 101 / 115.
 constexpr long kPagedTarget = 512;
-constexpr int kMinSplitSlots = 256;  // slots of a split at least (by capacity)
+// Slots of a split at least, and in bfloat16 one more for every 32 query rows of the launch: the partials of a split
+// are written and read by row, what it saves goes by its slots (in float32 by 8 times as much). 8 sequences of 128 tokens, 32 / 8 heads, windows
+// of 256 / 512 / 1024: 29.1 / 35.2 / 46.8 us, 39.7 / 43.7 / 51.7 without the second term; half of it 28.8 / 35.0 / 52.8.
+constexpr int kMinSplitSlots = 256;
+constexpr long kSplitRows = 32;
 constexpr float kSlack = 8.f;  // see paged_body
 constexpr int kHidden = 0x7fffffff;  // position of a slot whose page is missing
 
@@ -953,6 +957,11 @@ struct PagedPlan {
 
 // Workgroups for the split of a launch without long chunks: one a CU.
 constexpr long kFewTarget = 256;
+// Slots up to which two halves take less than splits and the launch that joins them, where the splits could be more
+// than two (bfloat16, head_dim 128: in float32 the scores, which both halves form, bound it). Decode steps of 32 / 8
+// heads, 8 / 4 / 2 / 1 sequences of 1024 slots 11.6 / 10.0 / 11.2 / 10.5 us, split 14.3 / 12.5 / 11.7 / 10.4; 4 / 1 of
+// 2048 slots 15.6 / 14.8, split 13.0 / 11.6.
+constexpr long kHalvesReach = 1024;
 // Slots of a split at most, whatever the number of workgroups: what one long sequence among many short ones
 // may hold up the launch by. Decode steps of 32 / 8 heads over 65536 slots of capacity, at 8192 / 16384 / 32768
 // slots a split / no such bound: 63 sequences of 1000 slots and one of 60000 182 / 219 / 335 / 571 us, 64 sequences
@@ -966,10 +975,11 @@ static PagedPlan paged_plan(const lg_paged_layer& l, const lg_page_map& m, long 
   p.many_tiles = 0;
   p.halves = 1;
   p.few = max_chunk * G <= kWaveRows;
-  long ns;
+  long ns, slots = kMinSplitSlots;
   if (p.few) {
     const long units = (long)m.batch * l.n_kv_heads;
     ns = kFewTarget / units;  // more than one a CU would run in two rounds
+    if (ns > 2 && reach <= kHalvesReach && l.dtype == LG_BF16 && l.head_dim == 128) ns = 2;
   } else {
     if (total * G > kWaveRows) {
       // a sequence of n rows has at most n / 128 + 1 tiles, and more than 32 rows
@@ -979,8 +989,9 @@ static PagedPlan paged_plan(const lg_paged_layer& l, const lg_page_map& m, long 
     }
     const long units = (p.many_tiles + m.batch) * l.n_kv_heads;
     ns = (kPagedTarget + units - 1) / units;
+    if (l.dtype == LG_BF16) slots += total * l.n_q_heads / kSplitRows;
   }
-  ns = std::min({ns, (reach + kMinSplitSlots - 1) / kMinSplitSlots, (long)kMaxNs});
+  ns = std::min({ns, (reach + slots - 1) / slots, (long)kMaxNs});
   const long least = std::min(reach / kMaxSplitSlotsPaged, (long)kMaxNs);
   if (p.few && ns == 2 && least < 2 && l.head_dim == 128) {
     ns = 1;
