@@ -50,6 +50,7 @@ namespace lg {
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -88,8 +89,9 @@ struct PagedAttendArgs {
 // without padding. The rows a lane reads differ from its first one by multiples that leave f as it is, so the
 // exchange is one xor with a constant on its first address (tiles lie at multiples of 1024 bytes).
 //
-// DV: the values of V that the workgroup forms outputs of, D or (KW = 8) half of them.
-template <typename T, int D, int KW, int DV = D>
+// DV: the values of V that the workgroup forms outputs of, D or (KW = 8) half of them. RW: rows of a matrix
+// instruction, 32 or (float32, KW > 1) 16.
+template <typename T, int D, int KW, int DV = D, int RW = 32>
 struct Team {
   static constexpr bool kF32 = sizeof(T) == 4;
   static constexpr int kRowBytes = D * (int)sizeof(T), kRowBytesV = DV * (int)sizeof(T);
@@ -109,7 +111,7 @@ struct Team {
   static constexpr int kLds = kTiles > kJoin ? kTiles : (kJoin + 511) & ~511;
   static __device__ __forceinline__ int fk(int row) { return kF32 || D == 128 ? row & 15 : (row >> 1) & 7; }
   static __device__ __forceinline__ int fv(int row) {
-    return kF32 ? 8 * ((row >> 2) & 1) : DV == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
+    return kF32 && RW == 16 ? 4 * ((row >> 2) & 3) : kF32 ? 8 * ((row >> 2) & 1) : DV == 128 ? 4 * (row & 3) : 4 * ((row >> 1) & 1);
   }
 };
 
@@ -125,6 +127,12 @@ constexpr int paged_lds() {
 template <typename T, int D, int KW, int DV>
 constexpr int few_lds() {
   return KW * (Team<T, D, KW, DV>::kLds + kRing) + 4 * KW;
+}
+
+// The value of lane ^ 16 (rows of 16 lanes change places in pairs).
+__device__ __forceinline__ float other_row(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float((threadIdx.x & 16) != 0 ? r[0] : r[1]);
 }
 
 // The value of lane ^ 32.
@@ -252,13 +260,26 @@ __device__ __forceinline__ bool skip_hidden(const PagedAttendArgs& a, Job& job, 
 }
 
 // flags: in LDS, one a team (see make_finite).
-template <typename T, int D, int KW, int DV>
+//
+// RW = 16 (float32, at most 16 rows): the same walk with v_mfma_f32_16x16x4. A lane holds 8 of 32 keys, 4 of every 16, and
+// the four lanes of a row are 16 apart. The float32 products bound a decode step: with 32 rows of which a few live they
+// cost twice as much. 8 sequences of 4096 / 16 of 8192 slots of capacity, 32 / 8 heads: 46.9 / 177 us, 56.9 / 245 with 32
+// rows; 16 tokens of a tiny layer 8.9, 11.1. (bfloat16 has no need: its decode steps are bound by memory.)
+//
+// The lane's values of S and O lie in fours: S at keys kFour i + 4 part, O at values RW d + kFour i + 4 part.
+template <typename T, int D, int KW, int DV, int RW = 32>
 __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, char* lds, int32_t* flags) {
-  using C = Team<T, D, KW, DV>;
+  using C = Team<T, D, KW, DV, RW>;
+  static_assert(RW == 32 || (C::kF32 && KW > 1), "16 rows: float32, few rows");
   constexpr bool F32 = C::kF32;
-  constexpr int NK = C::kKeys, NB = NK / 32, ND = DV / 32, RB = C::kRowBytes, RBV = C::kRowBytesV;
+  constexpr int NK = C::kKeys, NB = NK / 32, ND = DV / RW, RB = C::kRowBytes, RBV = C::kRowBytesV;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int half = lane >> 5, col = lane & 31;
+  const int part = lane / RW, col = lane % RW;
+  constexpr int kParts4 = 64 / RW, kFour = 4 * kParts4;  // lanes of a row; keys (values) between a lane's fours
+  constexpr int NS = RW / 2, NI = NS / 4;                // the lane's weights of 32 keys
+  constexpr int NO = RW * RW / 64, NOI = NO / 4;         // ... and values of an accumulator of O
+  using Weights = std::conditional_t<RW == 32, f32x16, f32x8>;
+  using Acc = std::conditional_t<RW == 32, f32x16, f32x4>;
   char* const my = KW > 1 ? lds + wave * (C::kLds + kRing) : lds;
   const MapArgs& m = a.map;
   const int32_t* const table = m.table + (size_t)job.b * m.P;
@@ -274,12 +295,12 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
   const int slot_q = job.base + tok;
   const bool idle = wrow0 >= job.rows;  // KW = 1: a wave without rows only loads
 
-  f32x16 O[ND];
+  Acc O[ND];
 #pragma unroll
   for (int d = 0; d < ND; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) O[d][i] = 0.f;
-  float mx = -INFINITY, l = 0.f, sfx = 0.f;  // l and sfx: the lane's half of the keys
+    for (int i = 0; i < NO; ++i) O[d][i] = 0.f;
+  float mx = -INFINITY, l = 0.f, sfx = 0.f;  // l and sfx: the lane's share of the keys
 
   int t_end = job.t_end, t_first = KW > 1 ? job.t_begin + wave : job.t_begin;
   const int last_slot =  // the last one that any row of the workgroup sees
@@ -300,14 +321,14 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
   };
   // What depends on the sequence alone is asked for together: the first tile's lookup, the queries, positions.
   if (t_first < t_end) look(t_first, ring);
-  // Q as the B operand: bf16: values 16 kk + 8 half ..; float32: values half D / 2 + 4 u ..
-  constexpr int NQ = F32 ? D / 8 : D / 16;
+  // Q as the B operand: bf16: values 16 kk + 8 part ..; float32: values part D / kParts4 + 4 u ..
+  constexpr int NQ = F32 ? D / (4 * kParts4) : D / 16;
   u32x4_t qf[NQ];
   {
     const char* src = (const char*)a.q + qrow * RB;
 #pragma unroll
     for (int i = 0; i < NQ; ++i)
-      qf[i] = *(const u32x4_t*)(src + (F32 ? half * (RB / 2) + 16 * i : 32 * i + 16 * half));
+      qf[i] = *(const u32x4_t*)(src + (F32 ? part * (RB / kParts4) + 16 * i : 32 * i + 16 * part));
   }
 
   const int p_q = pos[slot_q];
@@ -379,35 +400,51 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
   };
 
   // The lane's first addresses in a tile (see Team).
-  const int kx = col * RB + 16 * ((F32 ? half * (C::kRowPieces / 2) : half) ^ C::fk(col));
-  const int vx = F32 ? 4 * half * RBV + 16 * ((col >> 2) ^ C::fv(4 * half)) + 4 * (col & 3)
-                     : (4 * half + ((lane & 15) >> 2)) * RBV +
+  const int kx = col * RB + 16 * ((F32 ? part * (C::kRowPieces / kParts4) : part) ^ C::fk(col));
+  const int vx = F32 ? 4 * part * RBV + 16 * ((col >> 2) ^ C::fv(4 * part)) + 4 * (col & 3)
+                     : (4 * part + ((lane & 15) >> 2)) * RBV +
                            16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ C::fv((lane & 15) >> 2)) +
                            8 * (lane & 1);
 
   // S^T of 32 keys of a tile
-  auto scores = [&](const char* from, int k, f32x16& S) __attribute__((always_inline)) {
+  auto scores = [&](const char* from, int k, Weights& S) __attribute__((always_inline)) {
+    if constexpr (RW == 16) {
+      f32x4 s0 = {}, s1 = {};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) S[i] = 0.f;
+      for (int u = 0; u < NQ; ++u) {
+        const u32x4_t x = *(const u32x4_t*)(from + ((k + kx) ^ (16 * u)));
+        const u32x4_t y = *(const u32x4_t*)(from + ((k + kx) ^ (16 * u)) + 16 * RB);
 #pragma unroll
-    for (int u = 0; u < NQ; ++u) {
-      const u32x4_t x = *(const u32x4_t*)(from + ((k + kx) ^ (F32 ? 16 * u : 32 * u)));
-      if constexpr (F32) {
+        for (int e = 0; e < 4; ++e) {
+          s0 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x[e]), __uint_as_float(qf[u][e]), s0, 0, 0, 0);
+          s1 = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(y[e]), __uint_as_float(qf[u][e]), s1, 0, 0, 0);
+        }
+      }
+      S = Weights{s0[0], s0[1], s0[2], s0[3], s1[0], s1[1], s1[2], s1[3]};
+    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          S = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(qf[u][e]), S, 0, 0, 0);
-      } else {
-        S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, qf[u]),
-                                                    S, 0, 0, 0);
+      for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll
+      for (int u = 0; u < NQ; ++u) {
+        const u32x4_t x = *(const u32x4_t*)(from + ((k + kx) ^ (F32 ? 16 * u : 32 * u)));
+        if constexpr (F32) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            S = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(x[e]), __uint_as_float(qf[u][e]), S, 0, 0, 0);
+        } else {
+          S = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, qf[u]),
+                                                      S, 0, 0, 0);
+        }
       }
     }
   };
-  // Maximum of the lane's row over the block, both halves
-  auto top = [&](const f32x16& S) __attribute__((always_inline)) {
+  // Maximum of the lane's row over the block, in all its lanes
+  auto top = [&](const Weights& S) __attribute__((always_inline)) {
     float t4[4] = {S[0], S[1], S[2], S[3]};
 #pragma unroll
-    for (int i = 4; i < 16; ++i) t4[i & 3] = fmaxf(t4[i & 3], S[i]);
-    const float x = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+    for (int i = 4; i < NS; ++i) t4[i & 3] = fmaxf(t4[i & 3], S[i]);
+    float x = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+    if constexpr (RW == 16) x = fmaxf(x, other_row(x));
     return fmaxf(x, other_half(x));
   };
 
@@ -423,18 +460,18 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
     return __ballot(tp == kHidden) != 0 || s0 + NK - 1 > lo || (a.window > 0 && p_first <= hi && p_last >= a.n_sink);
   };
   auto four = [&](const int32_t* x, int nb, int i) __attribute__((always_inline)) {
-    return *(const i32x4*)(x + 32 * nb + 8 * i + 4 * half);
+    return *(const i32x4*)(x + 32 * nb + kFour * i + 4 * part);
   };
   auto set_bounds = [&]() __attribute__((always_inline)) {
     at[lane] = tp == kHidden ? INT32_MIN : a.window == 0 || tp < a.n_sink ? INT32_MAX : tp;
   };
-  auto mask = [&](f32x16& S, int nb) __attribute__((always_inline)) {
-    const int last = slot_q - s0 - 32 * nb - 4 * half;
+  auto mask = [&](Weights& S, int nb) __attribute__((always_inline)) {
+    const int last = slot_q - s0 - 32 * nb - 4 * part;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NI; ++i) {
       const i32x4 bound = four(at, nb, i);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) S[4 * i + j] = bound[j] > win && 8 * i + j <= last ? S[4 * i + j] : -INFINITY;
+      for (int j = 0; j < 4; ++j) S[4 * i + j] = bound[j] > win && kFour * i + j <= last ? S[4 * i + j] : -INFINITY;
     }
   };
   // The running maximum follows only when a score passes it by kSlack: weights are then at most 2^kSlack,
@@ -450,7 +487,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
 #pragma unroll
       for (int d = 0; d < ND; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) O[d][i] *= f;
+        for (int i = 0; i < NO; ++i) O[d][i] *= f;
     }
   };
   // The suffix's share of a tile: none, all, or slot by slot (slots that are not seen have weight 0)
@@ -460,19 +497,19 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
     const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
     return p_last <= suf_lo ? (int)kNone : p_first > suf_hi ? (int)kAll : (int)kSome;
   };
-  auto add_suffix = [&](const f32x16& P, int nb) __attribute__((always_inline)) {
+  auto add_suffix = [&](const Weights& P, int nb) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < NI; ++i) {
       const i32x4 p = four(at + 64, nb, i);
 #pragma unroll
       for (int j = 0; j < 4; ++j) sfx += p[j] > suf ? P[4 * i + j] : 0.f;
     }
   };
-  // S becomes the weights; returns their sum over the lane's half.
-  auto weights = [&](f32x16& S) __attribute__((always_inline)) {
+  // S becomes the weights; returns their sum over the lane's share.
+  auto weights = [&](Weights& S) __attribute__((always_inline)) {
     float s4[4];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < NS; ++i) {
       S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], a.scale_log2, mx == -INFINITY ? 0.f : -mx));
       s4[i & 3] = i < 4 ? S[i] : s4[i & 3] + S[i];
     }
@@ -501,8 +538,16 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
   };
 
   // O^T += V^T P^T over 32 keys
-  auto product = [&](const char* from, int v, const f32x16& P) __attribute__((always_inline)) {
-    if constexpr (F32) {
+  auto product = [&](const char* from, int v, const Weights& P) __attribute__((always_inline)) {
+    if constexpr (RW == 16) {
+#pragma unroll
+      for (int i = 0; i < NS; ++i)
+#pragma unroll
+        for (int d = 0; d < ND; ++d) {
+          const float x = *(const float*)(from + ((v + vx) ^ (64 * d)) + (kFour * (i >> 2) + (i & 3)) * RBV);
+          O[d] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, P[i], O[d], 0, 0, 0);
+        }
+    } else if constexpr (F32) {
 #pragma unroll
       for (int i = 0; i < 16; ++i)
 #pragma unroll
@@ -559,7 +604,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
       }
       look(t + 2, ring_to);
       if (idle || s0 > slot_hi) return;
-      f32x16 S, S1;
+      Weights S, S1;
       scores(from, here, S);
       if constexpr (NB > 1) {
         scores(from, here + kBlock, S1);
@@ -600,7 +645,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
       tile(t, ((t - t_first) & 1) * C::kBuffer, my, my, gr, ring + 128 * n2);
     }
   } else {
-    auto behind_scores = [&](int t, bool more, const Groups& gr, f32x16& S, const char* __restrict__ from,
+    auto behind_scores = [&](int t, bool more, const Groups& gr, Weights& S, const char* __restrict__ from,
                              char* __restrict__ to, int32_t* __restrict__ ring_to) __attribute__((always_inline)) {
       if (more) load_k(gr, to, 0);
       look(t + 2 * KW, ring_to);
@@ -630,7 +675,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
       at = ring + 128 * n;
       tp = place(at);
       s0 = slot_of(t);
-      f32x16 S;
+      Weights S;
       scores(my, 0, S);
       reads_done();
       behind_scores(t, more, gr, S, my, my, ring + 128 * n2);
@@ -654,18 +699,22 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
         if (!is_page(m, page) || s0 + key > slot_q || (a.window > 0 && pos[j] <= win && pos[j] >= a.n_sink)) continue;
         const T* row = (const T*)a.v +
                        ((((size_t)page * a.Hkv + job.h) << m.shift) + (j & ((1 << m.shift) - 1))) * D +
-                       job.d0 + 4 * half;
+                       job.d0 + 4 * part;
 #pragma unroll
         for (int d = 0; d < ND; ++d)
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const float x = (float)row[32 * d + 8 * (e >> 2) + (e & 3)];
+          for (int e = 0; e < NO; ++e) {
+            const float x = (float)row[RW * d + kFour * (e >> 2) + (e & 3)];
             O[d][e] += odd_bits(__float_as_uint(x), true) ? x : 0.f;
           }
       }
     }
   }
 
+  if constexpr (RW == 16) {
+    l += other_row(l);
+    sfx += other_row(sfx);
+  }
   l += other_half(l);
   sfx += other_half(sfx);
 
@@ -677,9 +726,9 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
       for (int d = 0; d < ND; ++d)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          *(f32x4*)(a.po + at * D + 32 * d + 8 * i + 4 * half) =
+          *(f32x4*)(a.po + at * D + 32 * d + 8 * i + 4 * part) =
               f32x4{O[d][4 * i], O[d][4 * i + 1], O[d][4 * i + 2], O[d][4 * i + 3]};
-      if (half == 0) *(f32x4*)(a.pml + at * 4) = f32x4{mx, l, sfx, 0.f};
+      if (part == 0) *(f32x4*)(a.pml + at * 4) = f32x4{mx, l, sfx, 0.f};
       return;
     }
     const float inv = l > 0.f || l != l ? 1.f / l : 0.f;  // no slot seen: 0
@@ -688,7 +737,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
     for (int d = 0; d < ND; ++d)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int at = 32 * d + 8 * i + 4 * half;
+        const int at = 32 * d + 8 * i + 4 * part;
         float x[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = l == 0.f ? 0.f : O[d][4 * i + e] * inv;
@@ -697,7 +746,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
         else
           *(u32x2_t*)(dst + at) = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
       }
-    if (half == 0) {
+    if (part == 0) {
       a.lse[qrow] = l == 0.f ? -INFINITY : kLn2 * (mx + __builtin_amdgcn_logf(l));
       const float mass = l == 0.f ? 0.f : sfx * inv;
       if (a.suffix != nullptr) a.suffix[qrow] = mass;
@@ -711,16 +760,16 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
 #pragma unroll
     for (int d = 0; d < ND; ++d)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *(f32x4*)(num + col * (DV + 4) + 32 * d + 8 * i + 4 * half) =
+      for (int i = 0; i < NOI; ++i)
+        *(f32x4*)(num + col * (DV + 4) + RW * d + kFour * i + 4 * part) =
             f32x4{O[d][4 * i], O[d][4 * i + 1], O[d][4 * i + 2], O[d][4 * i + 3]};
-    if (half == 0) {
+    if (part == 0) {
       num[kStat + col] = mx;
       num[kStat + kWaveRows + col] = l;
       num[kStat + 2 * kWaveRows + col] = sfx;
     }
     __syncthreads();
-    const int r = tid / kParts, part = tid % kParts;
+    const int r = tid / kParts, share = tid % kParts;
     if (job.row0 + r >= job.rows) return;
     float wm[KW], M = -INFINITY;
 #pragma unroll
@@ -738,15 +787,15 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
       L += f * src[kStat + kWaveRows + r];
       SF += f * src[kStat + 2 * kWaveRows + r];
 #pragma unroll
-      for (int i = 0; i < kChunks; ++i) x[i] += f * *(const f32x4*)(src + r * (DV + 4) + 4 * (kParts * i + part));
+      for (int i = 0; i < kChunks; ++i) x[i] += f * *(const f32x4*)(src + r * (DV + 4) + 4 * (kParts * i + share));
     }
     const int tk = (job.row0 + r) / a.G, gg = job.row0 + r - tk * a.G;
     const size_t row = (size_t)(job.first + tk) * a.Hq + job.h * a.G + gg;
-    const bool first = part == 0 && job.d0 == 0;  // the row's statistics
+    const bool first = share == 0 && job.d0 == 0;  // the row's statistics
     if (a.ns > 1) {
       const size_t at = (size_t)job.split * a.total * a.Hq + row;
 #pragma unroll
-      for (int i = 0; i < kChunks; ++i) *(f32x4*)(a.po + at * D + job.d0 + 4 * (kParts * i + part)) = x[i];
+      for (int i = 0; i < kChunks; ++i) *(f32x4*)(a.po + at * D + job.d0 + 4 * (kParts * i + share)) = x[i];
       if (first) *(f32x4*)(a.pml + at * 4) = f32x4{M, L, SF, 0.f};
       return;
     }
@@ -758,9 +807,9 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = L == 0.f ? 0.f : x[i][e] * inv;
       if constexpr (F32)
-        *(f32x4*)(dst + 4 * (kParts * i + part)) = y;
+        *(f32x4*)(dst + 4 * (kParts * i + share)) = y;
       else
-        *(u32x2_t*)(dst + 4 * (kParts * i + part)) = u32x2_t{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+        *(u32x2_t*)(dst + 4 * (kParts * i + share)) = u32x2_t{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
     }
     if (first) {
       a.lse[row] = L == 0.f ? -INFINITY : kLn2 * (M + __builtin_amdgcn_logf(L));
@@ -854,7 +903,7 @@ __global__ __launch_bounds__(kPagedThreads, (sizeof(T) == 4 && D == 128 ? 1 : 2)
 // For the 128 pairs of the decode step above 26.4 us a call, 34.4 with four-wave workgroups, four splits and the
 // launch that joins them (24 and 8 us).
 // Grid: (Hkv, ns, B) flattened into units; with two halves, groups of 8 units' first halves, then their second.
-template <typename T, int D, int KW, int DV>
+template <typename T, int D, int KW, int DV, int RW>
 __global__ __launch_bounds__(64 * KW) void paged_few(PagedAttendArgs a) {
   __shared__ __align__(512) char lds[few_lds<T, D, KW, DV>()];
   const unsigned per = (unsigned)(a.Hkv * a.ns);
@@ -870,7 +919,7 @@ __global__ __launch_bounds__(64 * KW) void paged_few(PagedAttendArgs a) {
   job.h = x % a.Hkv;
   if (!few_job(a, job, b, x == 0 && job.d0 == 0)) return;
   job_tiles<32>(a, job, kWaveRows, x / a.Hkv);
-  paged_body<T, D, KW, DV>(a, job, lds, (int32_t*)(lds + few_lds<T, D, KW, DV>() - 4 * KW));
+  paged_body<T, D, KW, DV, RW>(a, job, lds, (int32_t*)(lds + few_lds<T, D, KW, DV>() - 4 * KW));
 }
 
 // Joins the splits of a row: D / 4 lanes a query row of a token, four values each. What it reads of the partials
@@ -1044,15 +1093,24 @@ size_t paged_attend_bytes(const lg_paged_layer& l, const lg_page_map& m, int tot
   return align_up(most, 16);
 }
 
+template <typename T, int D, int KW, int RW>
+static void launch_few(const PagedAttendArgs& a, const PagedPlan& p, dim3 grid, hipStream_t st) {
+  if (p.halves == 1)
+    hipLaunchKernelGGL((paged_few<T, D, KW, D, RW>), grid, dim3(64 * KW), 0, st, a);
+  else if constexpr (D == 128)
+    hipLaunchKernelGGL((paged_few<T, D, KW, D / 2, RW>), grid, dim3(64 * KW), 0, st, a);
+}
+
 template <typename T, int D>
 static void launch_typed(const PagedAttendArgs& a, const PagedPlan& p, dim3 grid, hipStream_t st) {
   constexpr int KW = sizeof(T) == 4 && D == 128 ? 4 : 8;
-  if (!p.few)
+  if (!p.few) {
     hipLaunchKernelGGL((paged_attend<T, D>), grid, dim3(kPagedThreads), 0, st, a);
-  else if (p.halves == 1)
-    hipLaunchKernelGGL((paged_few<T, D, KW, D>), grid, dim3(64 * KW), 0, st, a);
-  else if constexpr (D == 128)
-    hipLaunchKernelGGL((paged_few<T, D, KW, D / 2>), grid, dim3(64 * KW), 0, st, a);
+  } else if (sizeof(T) == 4 && (long)a.max_chunk * a.G <= 16) {
+    launch_few<T, D, KW, sizeof(T) == 4 ? 16 : 32>(a, p, grid, st);
+  } else {
+    launch_few<T, D, KW, 32>(a, p, grid, st);
+  }
   const long rows = (long)a.total * a.Hq;
   if (p.ns > 1)
     hipLaunchKernelGGL((paged_join<T, D>), dim3((unsigned)((rows + join_rows<D>() - 1) / join_rows<D>())), dim3(kPagedThreads), 0,
