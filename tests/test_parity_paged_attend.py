@@ -184,6 +184,25 @@ def test_decode_batches(dtype, D, hq, hkv, batch):
     w.check()
 
 
+@pytest.mark.parametrize("dtype,D,hq,hkv,have,n", [
+    (BF, 128, 8, 2, [950, 3, 500], [1, 1, 1]),         # few pairs, a short cache: two workgroups share a row's outputs
+    (BF, 128, 4, 1, [700], [8]),
+    (BF, 128, 8, 2, [1100, 3, 500], [1, 1, 1]),        # a little longer: splits
+    (F32, 128, 8, 2, [950, 3, 500], [1, 4, 4]),        # 16 rows
+    (F32, 128, 8, 2, [950, 3, 500], [5, 1, 0]),        # 20
+    (F32, 64, 16, 4, [300, 33], [8, 1]),               # 32
+    (F32, 64, 16, 1, [300, 33], [1, 1]),               # 16
+    (F32, 64, 5, 1, [40, 0], [6, 3]),                  # 30 and 15
+    (F32, 128, 2, 1, [130] * 70, [16] + [9] * 69),     # 32 and 18, halves
+    (F32, 128, 3, 3, [90] * 40, [16] + [1] * 39),      # 16 and 1, halves
+])
+def test_few_rows(dtype, D, hq, hkv, have, n):
+    """Steps without long chunks at the edges of their launches: rows of a matrix instruction, halves and splits."""
+    a = Attend(dtype, D, hq, hkv, 16, have, n, seed=sum(n) + D)
+    a.call()
+    a.check(tokens=np.array([0, 1, 3, 4, -1]))
+
+
 def test_long_capacity():
     """More slots of capacity than a split may have: the launch splits rows though it has workgroups enough, and
     most splits are empty."""
