@@ -218,6 +218,10 @@ struct ForkArgs {
 constexpr int kForkThreads = 256;
 constexpr int kForkSlots = 1024;  // of capacity for a workgroup ...
 constexpr int kForkSpread = 64;   // ... up to this many a sequence
+// Slots of capacity of all sequences up to which one workgroup takes both steps: a call 4.7 us for 4 x 256 slots and
+// 6.0 for 8 x 1024, in two launches 7.5 and 7.8 (4 us of it the host's second launch); in a graph 3.7 / 6.3 against 5.2 /
+// 6.3, and behind from there on (8.7 against 6.3 for 8 x 2048).
+constexpr long kForkSmall = 8192;
 
 __device__ __forceinline__ bool fork_changes(const ForkArgs& a, int b, int* parent) {
   const int p = a.parent[b];
@@ -225,17 +229,13 @@ __device__ __forceinline__ bool fork_changes(const ForkArgs& a, int b, int* pare
   return p != b && p >= -1 && p < a.map.B;
 }
 
-// First launch: what each changed sequence becomes goes to the workspace (its parent may change too), and
-// the pages it will share are counted. Second launch: the references it held are given back, and it
-// becomes what the workspace holds. A page is never seen at zero in between.
-// Each thread of the second launch reads only what the first one wrote and the one entry that it replaces
-// itself, so a sequence's row can be split freely: a workgroup takes kForkSlots slots of the capacity.
-// The bytes (a few hundred KB) are nothing; what bounds it is two launches and one dependent read each.
-// Measured in a graph, both launches: 5.6 us for 4 x 256 slots, 6.5 for 32 x 2048, 7.1 for 4 x 16384;
-// with one workgroup a sequence 5.6, 8.0 and 29.6.
-__global__ __launch_bounds__(kForkThreads) void fork_read(ForkArgs a) {
+// First step: what each changed sequence becomes goes to the workspace (its parent may change too), and the
+// pages it will share are counted. Second step: the references it held are given back, and it becomes what the
+// workspace holds. A page is never seen at zero in between. A thread of the second step reads only what the
+// first one wrote and the one entry that it replaces itself, so a sequence's row can be split freely.
+// t: one of the `step` threads that work on b.
+__device__ __forceinline__ void fork_read_one(const ForkArgs& a, int b, int t, int step) {
   const MapArgs& m = a.map;
-  const int b = blockIdx.x, t = blockIdx.y * kForkThreads + threadIdx.x, step = gridDim.y * kForkThreads;
   int p;
   if (!fork_changes(a, b, &p) || p < 0) return;
   const int n = min(max(m.len[p], 0), m.cap);
@@ -244,14 +244,12 @@ __global__ __launch_bounds__(kForkThreads) void fork_read(ForkArgs a) {
     a.ws.table[(size_t)b * m.P + c] = page;
     if (is_page(m, page)) atomicAdd(m.ref + page, 1);
   }
-  for (int j = t; j < n; j += step)
-    a.ws.fresh[(size_t)b * m.cap + j] = m.pos[(size_t)p * m.cap + j];
+  for (int j = t; j < n; j += step) a.ws.fresh[(size_t)b * m.cap + j] = m.pos[(size_t)p * m.cap + j];
   if (t == 0) a.ws.src[b] = n;
 }
 
-__global__ __launch_bounds__(kForkThreads) void fork_write(ForkArgs a) {
+__device__ __forceinline__ void fork_write_one(const ForkArgs& a, int b, int t, int step) {
   const MapArgs& m = a.map;
-  const int b = blockIdx.x, t = blockIdx.y * kForkThreads + threadIdx.x, step = gridDim.y * kForkThreads;
   int p;
   if (!fork_changes(a, b, &p)) return;
   const int n = p < 0 ? 0 : a.ws.src[b];
@@ -261,9 +259,26 @@ __global__ __launch_bounds__(kForkThreads) void fork_write(ForkArgs a) {
     if (is_page(m, page)) atomicSub(m.ref + page, 1);
     m.table[at] = p < 0 ? -1 : a.ws.table[at];
   }
-  for (int j = t; j < n; j += step)
-    m.pos[(size_t)b * m.cap + j] = a.ws.fresh[(size_t)b * m.cap + j];
+  for (int j = t; j < n; j += step) m.pos[(size_t)b * m.cap + j] = a.ws.fresh[(size_t)b * m.cap + j];
   if (t == 0) m.len[b] = n;
+}
+
+// A launch a step; a workgroup takes kForkSlots slots of a sequence's capacity. The bytes (a few hundred KB) are
+// nothing; what bounds it is two launches and one dependent read each. Measured in a graph, both launches: 6.4 us
+// for 8 x 1024 slots, 6.5 for 32 x 2048, 7.1 for 4 x 16384; with one workgroup a sequence 6.4, 8.0 and 29.6.
+__global__ __launch_bounds__(kForkThreads) void fork_read(ForkArgs a) {
+  fork_read_one(a, blockIdx.x, blockIdx.y * kForkThreads + threadIdx.x, gridDim.y * kForkThreads);
+}
+__global__ __launch_bounds__(kForkThreads) void fork_write(ForkArgs a) {
+  fork_write_one(a, blockIdx.x, blockIdx.y * kForkThreads + threadIdx.x, gridDim.y * kForkThreads);
+}
+
+// Both steps of a small map in one workgroup and launch.
+__global__ __launch_bounds__(kMapThreads) void fork_small(ForkArgs a) {
+  const int t = threadIdx.x % kForkThreads, step = kMapThreads / kForkThreads;
+  for (int b = threadIdx.x / kForkThreads; b < a.map.B; b += step) fork_read_one(a, b, t, kForkThreads);
+  __syncthreads();
+  for (int b = threadIdx.x / kForkThreads; b < a.map.B; b += step) fork_write_one(a, b, t, kForkThreads);
 }
 
 // ------------------------------------------------------------------------------------------
@@ -523,6 +538,10 @@ hipError_t launch_fork(const lg_page_map& map, const int32_t* parent, void* ws, 
   a.map = map_args(map);
   a.ws = page_ws(map, ws);
   a.parent = parent;
+  if ((long)map.batch * a.map.cap <= kForkSmall) {
+    hipLaunchKernelGGL(fork_small, dim3(1), dim3(kMapThreads), 0, st, a);
+    return hipGetLastError();
+  }
   const dim3 grid(map.batch, (unsigned)min((a.map.cap - 1) / kForkSlots + 1, kForkSpread));
   hipLaunchKernelGGL(fork_read, grid, dim3(kForkThreads), 0, st, a);
   hipError_t e = hipGetLastError();
