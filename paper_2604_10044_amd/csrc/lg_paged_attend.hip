@@ -18,7 +18,7 @@
 //           V then comes from LDS four times as often as from the L2.
 //   KW > 1  the others (a decode step: G rows): the waves take every KW-th tile of 32 slots, each with LDS of its
 //           own and no barrier, and their (m, l, O) are joined at the end. paged_few is the launch for steps that
-//           have no others, 8 waves a workgroup; beside long chunks it is four (paged_attend).
+//           have no others, 8 waves a workgroup; beside long chunks (paged_attend) see side_waves.
 // When these workgroups are fewer than the CUs hold, the slots of a row are split over several and a second
 // launch joins them (paged_plan).
 //
@@ -32,7 +32,7 @@
 // TB/s: the memory. 4096 tokens of 32 / 8 heads behind 4096, 412 GFLOP, 433 to 474 us by card, 870 to 950
 // TFLOP/s: of a wave's time a third is matrix instructions and as much the exponentials with their maxima, sums
 // and roundings, which the other wave of its SIMD covers in part; the rest is issuing loads and scalar code.
-// float32 runs at 107 of the 154 TFLOP/s of a float32 product. 128 tokens each of four sequences with a window
+// float32 runs at 118 of the 154 TFLOP/s of a float32 product. 128 tokens each of four sequences with a window
 // of 2048 beside 12 decoding ones, 147 MB: 55 to 60 us, the length of a workgroup's chain of 17 tiles and the
 // launch that joins two splits.
 //
@@ -118,9 +118,17 @@ struct Team {
 // Tiles whose table entries and positions (64 of each) a wave holds at once.
 constexpr int kRing = 3 * 512;
 
+// Waves for a sequence of few rows beside long chunks; the other waves of the workgroup end at once (a barrier waits for
+// those that are left). Two in float32 with rows of 512 bytes: a workgroup then has 70 KB of LDS, and two of them on a CU
+// carry long chunks faster than one with 134 KB: 256 tokens each of 4 sequences of 4096 slots, 32 / 8 heads, 459 us
+// against 506, 16 sequences of which 4 bring 128 tokens to a window of 1024 116 against 138; steps whose decoding
+// sequences weigh most lose (8 sequences of 2048 slots, two bring 64 tokens: 99 against 92).
+template <typename T, int D>
+constexpr int side_waves() { return sizeof(T) == 4 && D == 128 ? 2 : 4; }
+
 template <typename T, int D>
 constexpr int paged_lds() {
-  constexpr int many = Team<T, D, 1>::kLds + 4 * kRing, few = 4 * (Team<T, D, 4>::kLds + kRing);
+  constexpr int many = Team<T, D, 1>::kLds + 4 * kRing, few = side_waves<T, D>() * (Team<T, D, side_waves<T, D>()>::kLds + kRing);
   return (many > few ? many : few) + 4 * 4;  // and the flags of make_finite
 }
 
@@ -841,7 +849,7 @@ __device__ __forceinline__ bool few_job(const PagedAttendArgs& a, Job& job, int 
 // sequence are Hkv apart, so with 8 heads (the XCDs are dealt workgroups in turn) they share an L2. The
 // tiles of many rows come first, the last of a sequence (the longest) before the others.
 template <typename T, int D>
-__global__ __launch_bounds__(kPagedThreads, (sizeof(T) == 4 && D == 128 ? 1 : 2)) void paged_attend(PagedAttendArgs a) {
+__global__ __launch_bounds__(kPagedThreads, 2) void paged_attend(PagedAttendArgs a) {
   __shared__ __align__(512) char lds[paged_lds<T, D>()];
   int32_t* const flags = (int32_t*)(lds + paged_lds<T, D>() - 16);
   const int per = a.Hkv * a.ns;
@@ -889,10 +897,17 @@ __global__ __launch_bounds__(kPagedThreads, (sizeof(T) == 4 && D == 128 ? 1 : 2)
     paged_body<T, D, 1, D>(a, job, lds, flags);
     return;
   }
-  if (few_job(a, job, unit - a.many_tiles, rest == 0)) {
-    job_tiles<Team<T, D, 4>::kKeys>(a, job, kWaveRows, split);
+  constexpr int KW = side_waves<T, D>();
+  if (few_job(a, job, unit - a.many_tiles, rest == 0) && threadIdx.x < 64 * KW) {
+    job_tiles<Team<T, D, KW>::kKeys>(a, job, kWaveRows, split);
     job.d0 = 0;
-    paged_body<T, D, 4, D>(a, job, lds, flags);
+    if constexpr (sizeof(T) == 4) {
+      if (job.rows <= 16) {
+        paged_body<T, D, KW, D, 16>(a, job, lds, flags);
+        return;
+      }
+    }
+    paged_body<T, D, KW, D>(a, job, lds, flags);
   }
 }
 
