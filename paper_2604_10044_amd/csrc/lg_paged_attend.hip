@@ -32,7 +32,7 @@
 // TB/s: the memory. 4096 tokens of 32 / 8 heads behind 4096, 412 GFLOP, 433 to 474 us by card, 870 to 950
 // TFLOP/s: of a wave's time a third is matrix instructions and as much the exponentials with their maxima, sums
 // and roundings, which the other wave of its SIMD covers in part; the rest is issuing loads and scalar code.
-// float32 runs at 118 of the 154 TFLOP/s of a float32 product. 128 tokens each of four sequences with a window
+// float32 runs at 133 of the 154 TFLOP/s of a float32 product. 128 tokens each of four sequences with a window
 // of 2048 beside 12 decoding ones, 147 MB: 55 to 60 us, the length of a workgroup's chain of 17 tiles and the
 // launch that joins two splits.
 //
