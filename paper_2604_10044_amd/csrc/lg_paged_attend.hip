@@ -187,8 +187,17 @@ __device__ __forceinline__ bool odd_bits(uint32_t x, bool f32) {  // an infinity
 
 // conf[b] = max(conf[b], mass): masses are not negative, so their order is that of their bits; a NaN (of
 // whatever sign) makes it NaN.
-__device__ __forceinline__ void raise_conf(float* conf, float mass) {
-  atomicMax((int*)conf, mass != mass ? 0x7fc00000 : __float_as_int(mass));
+__device__ __forceinline__ int conf_bits(float mass) { return mass != mass ? 0x7fc00000 : __float_as_int(mass); }
+
+// For the lanes of a wave that are `mine`, of one sequence. The confidences of a batch lie in a few cache lines, where
+// atomics wait for each other: with one a row a decode step of 16 x 48 heads of 64 took 20.6 us, with one a wave, or a
+// workgroup and token in paged_join, 12.0.
+__device__ __forceinline__ void raise_conf(float* conf, float mass, bool mine) {
+  if (__ballot(mine) == 0) return;
+  int x = mine ? conf_bits(mass) : 0;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) x = max(x, __shfl_xor(x, o, 64));
+  if ((threadIdx.x & 63) == 0) atomicMax((int*)conf, x);
 }
 
 // Order for the scheduler: the scores of 64 keys' 16 reads of LDS and 16 matrix instructions, the reads 8
@@ -727,7 +736,11 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
   sfx += other_half(sfx);
 
   if constexpr (KW == 1) {
-    if (idle || !live) return;
+    if (idle) return;
+    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;  // no slot seen: 0
+    const float mass = l == 0.f ? 0.f : sfx * inv;
+    if (a.ns == 1 && a.conf != nullptr) raise_conf(a.conf + job.b, mass, tok == job.rows / a.G - 1);
+    if (!live) return;
     if (a.ns > 1) {
       const size_t at = (size_t)job.split * a.total * a.Hq + qrow;
 #pragma unroll
@@ -739,7 +752,6 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
       if (part == 0) *(f32x4*)(a.pml + at * 4) = f32x4{mx, l, sfx, 0.f};
       return;
     }
-    const float inv = l > 0.f || l != l ? 1.f / l : 0.f;  // no slot seen: 0
     T* dst = (T*)a.out + qrow * D;
 #pragma unroll
     for (int d = 0; d < ND; ++d)
@@ -756,10 +768,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
       }
     if (part == 0) {
       a.lse[qrow] = l == 0.f ? -INFINITY : kLn2 * (mx + __builtin_amdgcn_logf(l));
-      const float mass = l == 0.f ? 0.f : sfx * inv;
       if (a.suffix != nullptr) a.suffix[qrow] = mass;
-      if (a.conf != nullptr && tok == job.rows / a.G - 1)
-        raise_conf(a.conf + job.b, mass);
     }
   } else {
     // Join the waves: their numerators and statistics through LDS, 2 KW threads a row.
@@ -777,8 +786,39 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
       num[kStat + 2 * kWaveRows + col] = sfx;
     }
     __syncthreads();
+    auto row_of = [&](int r) __attribute__((always_inline)) {
+      const int tk = r / a.G;
+      return (size_t)(job.first + tk) * a.Hq + job.h * a.G + (r - tk * a.G);
+    };
+    const size_t split0 = (size_t)job.split * a.total * a.Hq;
+    if (wave == KW - 1 && job.d0 == 0) {  // the statistics, a lane a row
+      const int r = min(col, job.rows - 1);
+      float M = -INFINITY, L = 0.f, SF = 0.f;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) M = fmaxf(M, ((const float*)(lds + w * (C::kLds + kRing)))[kStat + r]);
+      const float Ms = M == -INFINITY ? 0.f : M;
+#pragma unroll
+      for (int w = 0; w < KW; ++w) {
+        const float* src = (const float*)(lds + w * (C::kLds + kRing)) + kStat + r;
+        const float f = __builtin_amdgcn_exp2f(src[0] - Ms);
+        L += f * src[kWaveRows];
+        SF += f * src[2 * kWaveRows];
+      }
+      const bool own = lane < job.rows;
+      const size_t row = row_of(r);
+      if (a.ns > 1) {
+        if (own) *(f32x4*)(a.pml + (split0 + row) * 4) = f32x4{M, L, SF, 0.f};
+      } else {
+        const float mass = L == 0.f ? 0.f : SF * (1.f / L);
+        if (own) {
+          a.lse[row] = L == 0.f ? -INFINITY : kLn2 * (M + __builtin_amdgcn_logf(L));
+          if (a.suffix != nullptr) a.suffix[row] = mass;
+        }
+        if (a.conf != nullptr) raise_conf(a.conf + job.b, mass, r / a.G == job.rows / a.G - 1);
+      }
+    }
     const int r = tid / kParts, share = tid % kParts;
-    if (job.row0 + r >= job.rows) return;
+    if (r >= job.rows) return;
     float wm[KW], M = -INFINITY;
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
@@ -786,25 +826,21 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
       M = fmaxf(M, wm[w]);
     }
     const float Ms = M == -INFINITY ? 0.f : M;
-    float L = 0.f, SF = 0.f;
+    float L = 0.f;
     f32x4 x[kChunks] = {};
 #pragma unroll
     for (int w = 0; w < KW; ++w) {
       const float* src = (const float*)(lds + w * (C::kLds + kRing));
       const float f = __builtin_amdgcn_exp2f(wm[w] - Ms);
       L += f * src[kStat + kWaveRows + r];
-      SF += f * src[kStat + 2 * kWaveRows + r];
 #pragma unroll
       for (int i = 0; i < kChunks; ++i) x[i] += f * *(const f32x4*)(src + r * (DV + 4) + 4 * (kParts * i + share));
     }
-    const int tk = (job.row0 + r) / a.G, gg = job.row0 + r - tk * a.G;
-    const size_t row = (size_t)(job.first + tk) * a.Hq + job.h * a.G + gg;
-    const bool first = share == 0 && job.d0 == 0;  // the row's statistics
+    const size_t row = row_of(r);
     if (a.ns > 1) {
-      const size_t at = (size_t)job.split * a.total * a.Hq + row;
 #pragma unroll
-      for (int i = 0; i < kChunks; ++i) *(f32x4*)(a.po + at * D + job.d0 + 4 * (kParts * i + share)) = x[i];
-      if (first) *(f32x4*)(a.pml + at * 4) = f32x4{M, L, SF, 0.f};
+      for (int i = 0; i < kChunks; ++i)
+        *(f32x4*)(a.po + (split0 + row) * D + job.d0 + 4 * (kParts * i + share)) = x[i];
       return;
     }
     const float inv = 1.f / L;
@@ -818,12 +854,6 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
         *(f32x4*)(dst + 4 * (kParts * i + share)) = y;
       else
         *(u32x2_t*)(dst + 4 * (kParts * i + share)) = u32x2_t{pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
-    }
-    if (first) {
-      a.lse[row] = L == 0.f ? -INFINITY : kLn2 * (M + __builtin_amdgcn_logf(L));
-      const float mass = L == 0.f ? 0.f : SF * inv;
-      if (a.suffix != nullptr) a.suffix[row] = mass;
-      if (a.conf != nullptr && tk == job.rows / a.G - 1) raise_conf(a.conf + job.b, mass);
     }
   }
 }
@@ -948,8 +978,10 @@ constexpr int join_rows() { return kPagedThreads / (D / 4); }
 
 template <typename T, int D>
 __global__ __launch_bounds__(kPagedThreads) void paged_join(PagedAttendArgs a) {
+  __shared__ int best[join_rows<D>()];  // of the tokens that the workgroup has rows of
   const long long rows = (long long)a.total * a.Hq;
   const long long first = (long long)blockIdx.x * join_rows<D>();
+  if (threadIdx.x < join_rows<D>()) best[threadIdx.x] = -1;
   const long long row = min(first + threadIdx.x / (D / 4), rows - 1);
   const int d = threadIdx.x % (D / 4) * 4;
   f32x4 st[kJoinAhead], y[kJoinAhead];
@@ -991,9 +1023,21 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join(PagedAttendArgs a) {
       }
     M = top;
   }
-  if (first + threadIdx.x / (D / 4) >= rows) return;
-  if (r < c.first || r >= c.first + c.n || c.n > a.max_chunk || base < 0 || base > a.map.cap - c.n) return;
+  const bool live = first + threadIdx.x / (D / 4) < rows && r >= c.first && r < c.first + c.n && c.n <= a.max_chunk &&
+                    base >= 0 && base <= a.map.cap - c.n;
   const float inv = 1.f / L;
+  const float mass = L == 0.f ? 0.f : SF * inv;
+  if (a.conf != nullptr) {
+    const int at = r - (int)(first / a.Hq);  // below join_rows: a token has a row at least
+    const bool newest = live && r == c.first + c.n - 1;
+    __syncthreads();
+    if (d == 0 && newest) atomicMax(best + at, conf_bits(mass));
+    __syncthreads();
+    // the first thread of the token's first row here
+    const bool begins = row == first || row % a.Hq == 0;
+    if (d == 0 && newest && begins) atomicMax((int*)a.conf + b, best[at]);
+  }
+  if (!live) return;
 #pragma unroll
   for (int e = 0; e < 4; ++e) x[e] = L == 0.f ? 0.f : x[e] * inv;
   T* dst = (T*)a.out + row * D + d;
@@ -1003,9 +1047,7 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join(PagedAttendArgs a) {
     *(u32x2_t*)dst = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
   if (d == 0) {
     a.lse[row] = L == 0.f ? -INFINITY : kLn2 * (M + __builtin_amdgcn_logf(L));
-    const float mass = L == 0.f ? 0.f : SF * inv;
     if (a.suffix != nullptr) a.suffix[row] = mass;
-    if (a.conf != nullptr && r == c.first + c.n - 1) raise_conf(a.conf + b, mass);
   }
 }
 
