@@ -1066,8 +1066,9 @@ constexpr long kFewTarget = 256;
 // Slots up to which two halves take less than splits and the launch that joins them, where the splits could be more
 // than two (bfloat16, head_dim 128: in float32 the scores, which both halves form, bound it). Decode steps of 32 / 8
 // heads, 8 / 4 / 2 / 1 sequences of 1024 slots 11.6 / 10.0 / 11.2 / 10.5 us, split 14.3 / 12.5 / 11.7 / 10.4; 4 / 1 of
-// 2048 slots 15.6 / 14.8, split 13.0 / 11.6.
-constexpr long kHalvesReach = 1024;
+// 2048 slots 15.6 / 14.8, split 13.0 / 11.6. From 64 pairs of a sequence and a KV head on (three or four splits) further:
+// 16 / 20 sequences, 28 / 4 heads, 2048 slots 17.6 / 18.5, split 19.0 / 21.8; of 4096 26.5 / 28.8, split 25.4 / 30.0.
+constexpr long kHalvesReach = 1024, kHalvesReachMany = 2560, kHalvesMany = 64;
 // Slots of a split at most, whatever the number of workgroups: what one long sequence among many short ones
 // may hold up the launch by. Decode steps of 32 / 8 heads over 65536 slots of capacity, at 8192 / 16384 / 32768
 // slots a split / no such bound: 63 sequences of 1000 slots and one of 60000 182 / 219 / 335 / 571 us, 64 sequences
@@ -1085,7 +1086,7 @@ static PagedPlan paged_plan(const lg_paged_layer& l, const lg_page_map& m, long 
   if (p.few) {
     const long units = (long)m.batch * l.n_kv_heads;
     ns = kFewTarget / units;  // more than one a CU would run in two rounds
-    if (ns > 2 && reach <= kHalvesReach && l.dtype == LG_BF16 && l.head_dim == 128) ns = 2;
+    if (ns > 2 && reach <= (units < kHalvesMany ? kHalvesReach : kHalvesReachMany) && l.dtype == LG_BF16 && l.head_dim == 128) ns = 2;
   } else {
     if (total * G > kWaveRows) {
       // a sequence of n rows has at most n / 128 + 1 tiles, and more than 32 rows
