@@ -536,6 +536,16 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
   // share the tile, so each that reads it does this first when any of them has to, all with the same result:
   // what a wave then reads does not depend on the others' pace.
   auto make_finite = [&](char* v) __attribute__((always_inline)) {
+    // Is there any? An exponent of ones and one more carries into the bit above it.
+    constexpr uint32_t kExp = F32 ? 0x7f800000u : 0x7f807f80u, kOne = F32 ? 0x00800000u : 0x00800080u;
+    uint32_t carry = 0;
+#pragma unroll
+    for (int i = 0; i < C::kTileV / 1024; ++i) {
+      const u32x4_t x = *(const u32x4_t*)(v + 1024 * i + 16 * lane);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) carry |= (x[e] & kExp) + kOne;
+    }
+    if (!__any((carry & (kExp + kOne)) != 0)) return;
     for (int i = lane; i < C::kTileV / 16; i += 64) {
       u32x4_t x = *(const u32x4_t*)(v + 16 * i);
       if (odd_bits(x[0], F32) || odd_bits(x[1], F32) || odd_bits(x[2], F32) || odd_bits(x[3], F32)) {
