@@ -33,8 +33,8 @@
 // TFLOP/s: of a wave's time a third is matrix instructions and as much the exponentials with their maxima, sums
 // and roundings, which the other wave of its SIMD covers in part; the rest is issuing loads and scalar code.
 // float32 runs at 133 of the 154 TFLOP/s of a float32 product. 128 tokens each of four sequences with a window
-// of 2048 beside 12 decoding ones, 147 MB: 55 to 60 us, the length of a workgroup's chain of 17 tiles and the
-// launch that joins two splits.
+// of 2048 beside 12 decoding ones, 147 MB: 54 to 58 us: a workgroup's chain (4 us to its first tile, 17 tiles of 1.7 us
+// and 1.4 more for each of the two or three that are masked) and the launch that joins two splits.
 //
 // Tried and left: 8 waves sharing the tiles of 256 rows, one workgroup a CU (422 against 440 us for the 4096
 // tokens, but 85 against 54 for the mixed step and 177 against 163 for chunks of 512 at head_dim 64); tiles of 32
@@ -61,11 +61,13 @@ constexpr int kWaveRows = 32;
 constexpr int kManyRows = 128;   // rows of a KW = 1 workgroup
 constexpr int kPagedThreads = 256;
 // Workgroups a launch with long chunks aims for by splitting slots: two a CU. The mixed step above at 256 / 512 /
-// 1024: 72 / 58.6 / 61 us, 256 tokens behind 16128 slots 108 / 101 / 115.
+// 768 / 1024: 66.3 / 54.9 / 54.8 / 59.7 us, 256 tokens behind 16128 slots 109 / 101 at 256 / 512, 2048 behind 6144
+// 245 / 270 at 512 / 768.
 constexpr long kPagedTarget = 512;
 // Slots of a split at least, and in bfloat16 one more for every 32 query rows of the launch: the partials of a split
-// are written and read by row, what it saves goes by its slots (in float32 by 8 times as much). 8 sequences of 128 tokens, 32 / 8 heads, windows
-// of 256 / 512 / 1024: 29.1 / 35.2 / 46.8 us, 39.7 / 43.7 / 51.7 without the second term; half of it 28.8 / 35.0 / 52.8.
+// are written and read by row, what it saves goes by its slots (in float32 by 8 times as much). 8 sequences of 128
+// tokens, 32 / 8 heads, windows of 256 / 512 / 1024: 22.3 / 28.4 / 40.5 us, 38.7 / 41.7 / 49.5 without the second term;
+// half of it 22.6 / 28.9 / 51.7.
 constexpr int kMinSplitSlots = 256;
 constexpr long kSplitRows = 32;
 constexpr float kSlack = 8.f;  // see paged_body
@@ -255,7 +257,7 @@ __device__ __forceinline__ void job_tiles(const PagedAttendArgs& a, Job& job, in
 
 // Tiles behind the first tokens' that no row sees, by the window of the workgroup's first one: the first tile whose last
 // slot it sees, found by search, 64 probes a round. True if the share has changed. Without holes one read that the
-// first tile's lookup overlaps (59.6 us for the mixed step above, 60.2 without the search). 32 sequences of 8192 slots
+// first tile's lookup overlaps (no difference for the mixed step above). 32 sequences of 8192 slots
 // that decode with a window of 4096 over a history thinned out four to one: 58 us, 100 without.
 template <int NK>
 __device__ __forceinline__ bool skip_hidden(const PagedAttendArgs& a, Job& job, const int32_t* pos) {
@@ -280,8 +282,8 @@ __device__ __forceinline__ bool skip_hidden(const PagedAttendArgs& a, Job& job, 
 //
 // RW = 16 (float32, at most 16 rows): the same walk with v_mfma_f32_16x16x4. A lane holds 8 of 32 keys, 4 of every 16, and
 // the four lanes of a row are 16 apart. The float32 products bound a decode step: with 32 rows of which a few live they
-// cost twice as much. 8 sequences of 4096 / 16 of 8192 slots of capacity, 32 / 8 heads: 46.9 / 177 us, 56.9 / 245 with 32
-// rows; 16 tokens of a tiny layer 8.9, 11.1. (bfloat16 has no need: its decode steps are bound by memory.)
+// cost twice as much. 8 sequences of 4096 / 16 of 8192 slots of capacity, 32 / 8 heads: 44.8 / 179 us, 52.2 / 248 with 32
+// rows; 16 tokens of a tiny layer 8.6, 10.6. (bfloat16 has no need: its decode steps are bound by memory.)
 //
 // The lane's values of S and O lie in fours: S at keys kFour i + 4 part, O at values RW d + kFour i + 4 part.
 template <typename T, int D, int KW, int DV, int RW = 32>
@@ -1073,12 +1075,11 @@ struct PagedPlan {
 
 // Workgroups for the split of a launch without long chunks: one a CU.
 constexpr long kFewTarget = 256;
-// Slots up to which two halves take less than splits and the launch that joins them, where the splits could be more
-// than two (bfloat16, head_dim 128: in float32 the scores, which both halves form, bound it). Decode steps of 32 / 8
-// heads, 8 / 4 / 2 / 1 sequences of 1024 slots 11.6 / 10.0 / 11.2 / 10.5 us, split 14.3 / 12.5 / 11.7 / 10.4; 4 / 1 of
-// 2048 slots 15.6 / 14.8, split 13.0 / 11.6. From 64 pairs of a sequence and a KV head on (three or four splits) further:
-// 16 / 20 sequences, 28 / 4 heads, 2048 slots 17.6 / 18.5, split 19.0 / 21.8; of 4096 26.5 / 28.8, split 25.4 / 30.0.
-constexpr long kHalvesReach = 1024, kHalvesReachMany = 2560, kHalvesMany = 64;
+// Three or four splits (64 pairs of a sequence and a KV head on) take more than two halves without a join up to this many
+// slots (bfloat16, head_dim 128: in float32 the scores, which both halves form, bound it). Decode steps of 16 / 20
+// sequences, 28 / 4 heads, 2048 slots 17.3 / 18.2 us, split 18.5 / 20.9; 16 of 4096 slots 26.5, split 25.4. With fewer pairs
+// the two are within half a microsecond at 1024 slots and splits ahead behind that.
+constexpr long kHalvesReach = 2560, kHalvesPairs = 64;
 // Slots of a split at most, whatever the number of workgroups: what one long sequence among many short ones
 // may hold up the launch by. Decode steps of 32 / 8 heads over 65536 slots of capacity, at 8192 / 16384 / 32768
 // slots a split / no such bound: 63 sequences of 1000 slots and one of 60000 182 / 219 / 335 / 571 us, 64 sequences
@@ -1096,7 +1097,7 @@ static PagedPlan paged_plan(const lg_paged_layer& l, const lg_page_map& m, long 
   if (p.few) {
     const long units = (long)m.batch * l.n_kv_heads;
     ns = kFewTarget / units;  // more than one a CU would run in two rounds
-    if (ns > 2 && reach <= (units < kHalvesMany ? kHalvesReach : kHalvesReachMany) && l.dtype == LG_BF16 && l.head_dim == 128) ns = 2;
+    if (ns > 2 && units >= kHalvesPairs && reach <= kHalvesReach && l.dtype == LG_BF16 && l.head_dim == 128) ns = 2;
   } else {
     if (total * G > kWaveRows) {
       // a sequence of n rows has at most n / 128 + 1 tiles, and more than 32 rows

@@ -185,10 +185,10 @@ def test_decode_batches(dtype, D, hq, hkv, batch):
 
 
 @pytest.mark.parametrize("dtype,D,hq,hkv,have,n", [
-    (BF, 128, 8, 2, [950, 3, 500], [1, 1, 1]),         # few pairs, a short cache: two workgroups share a row's outputs
+    (BF, 128, 8, 2, [950, 3, 500], [1, 1, 1]),         # few pairs: splits
     (BF, 128, 4, 1, [700], [8]),
-    (BF, 128, 8, 2, [1100, 3, 500], [1, 1, 1]),        # a little longer: splits
-    (BF, 128, 8, 4, [1400] + [60] * 15, [1] * 16),     # 64 pairs: halves further up
+    (BF, 128, 8, 2, [1100, 3, 500], [1, 1, 1]),
+    (BF, 128, 8, 4, [1400] + [60] * 15, [1] * 16),     # 64 pairs: two workgroups share a row's outputs
     (F32, 128, 8, 2, [950, 3, 500], [1, 4, 4]),        # 16 rows
     (F32, 128, 8, 2, [950, 3, 500], [5, 1, 0]),        # 20
     (F32, 64, 16, 4, [300, 33], [8, 1]),               # 32
