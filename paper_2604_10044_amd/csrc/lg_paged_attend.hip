@@ -29,7 +29,7 @@
 //
 // What bounds it, measured on MI355X (a copy reaches 5.2 TB/s, a bfloat16 matrix product of 8192^3 1100
 // TFLOP/s): a decode step of 32 sequences of 28 / 4 heads and 1280 to 2047 slots, 112 MB, 23.2 us in a graph, 4.8
-// TB/s: the memory. 4096 tokens of 32 / 8 heads behind 4096, 412 GFLOP, 433 to 474 us by card, 870 to 950
+// TB/s: the memory. 4096 tokens of 32 / 8 heads behind 4096, 412 GFLOP, 421 to 474 us by card, 870 to 980
 // TFLOP/s: of a wave's time a third is matrix instructions and as much the exponentials with their maxima, sums
 // and roundings, which the other wave of its SIMD covers in part; the rest is issuing loads and scalar code.
 // float32 runs at 133 of the 154 TFLOP/s of a float32 product. 128 tokens each of four sequences with a window
