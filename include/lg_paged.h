@@ -183,9 +183,11 @@ size_t lg_paged_attend_workspace(const lg_paged_layer* layer, const lg_page_map*
  *                and p - window saturate.
  *   lse, suffix_mass [total][n_q_heads] float32; suffix_mass may be NULL; conf [batch] or NULL.
  *   workspace    16-byte aligned (LG_ERR_ALIGN, LG_ERR_WORKSPACE).
- * bfloat16 layers multiply alpha as bfloat16 with V (one rounding of each weight before the float32
- * sum); lse and suffix_mass are sums of the float32 weights. An infinity in v whose weight is so small that
- * it rounds to 0 gives a token that sees it that infinity or NaN. */
+ * bfloat16 layers: where a sequence's new tokens have at most 32 query heads of a KV head together (every
+ * decode step; n * n_q_heads / n_kv_heads <= 32), alpha multiplies V as two bfloat16 terms, within 2^-16 of
+ * it, as in lg_decode_attend; in longer chunks as one bfloat16 (one rounding, at most 2^-8 of it). The sums are
+ * float32, and lse and suffix_mass are sums of the float32 weights. An infinity in v whose weight is below
+ * 2^-100 of the row's largest gives a token that sees it that infinity or NaN. */
 lg_status lg_paged_attend(const lg_paged_layer* layer, const lg_page_map* map, const void* q,
                           void* out, const int32_t* q_start, const int32_t* base, int32_t total,
                           int32_t max_chunk, int32_t window, int32_t n_sink,

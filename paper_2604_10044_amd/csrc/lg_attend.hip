@@ -605,11 +605,6 @@ struct StashRow {
   bool use_lds;    // fixed per kernel instantiation
 };
 
-// The largest bfloat16 value below x, as a float's bits (x >= 0; 0 stays 0, NaN stays NaN).
-__device__ __forceinline__ uint32_t bf16_below(float x) {
-  return __builtin_elementwise_sub_sat(__float_as_uint(x), 1u) & 0xffff0000u;
-}
-
 // Second half: online softmax, logit stash, suffix mass, and alpha.V (DV dims), V from the LDS tile
 // (bfloat16) or from the block's registers (float32).
 // RC and bfloat16: alpha enters alpha.V as a whole float32, in three terms, and an infinite V value of a

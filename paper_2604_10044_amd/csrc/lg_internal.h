@@ -267,6 +267,11 @@ __device__ __forceinline__ uint16_t f32_to_bf16(float f) {
   return (uint16_t)((u + 0x7fffu + ((u >> 16) & 1u)) >> 16);
 }
 
+// The largest bfloat16 value below x, as a float's bits (x >= 0; 0 stays 0, NaN stays NaN).
+__device__ __forceinline__ uint32_t bf16_below(float x) {
+  return __builtin_elementwise_sub_sat(__float_as_uint(x), 1u) & 0xffff0000u;
+}
+
 // a - b saturated to the int32 range: thresholds on positions stay defined for any device-side
 // position and width a caller passes.
 __device__ __forceinline__ int sat_sub(int a, int b) {

@@ -9,7 +9,7 @@
 //   O^T = O^T 2^(m - m') + V^T P^T   A = V^T read transposed from LDS, B = P^T
 // With S transposed a lane holds 16 keys of ONE row (the accumulator of v_mfma_f32_32x32: column =
 // lane % 32, rows 8 i + 4 (lane / 32) + j), so the maximum and the sums are in the lane but for one exchange
-// with lane ^ 32, and the rounded P is the B operand of the second product as it lies in the registers:
+// with lane ^ 32, and P in bfloat16 is the B operand of the second product as it lies in the registers:
 // V^T is read in the same order of keys. Scores are in units of log 2 (exp2).
 //
 // Workgroups (template KW, waves along the keys):
@@ -28,7 +28,7 @@
 // are not finite count as 0 in it, and reach the rows that see them in a pass behind the loop.
 //
 // What bounds it, measured on MI355X (a copy reaches 5.2 TB/s, a bfloat16 matrix product of 8192^3 1100
-// TFLOP/s): a decode step of 32 sequences of 28 / 4 heads and 1280 to 2047 slots, 112 MB, 23.2 us in a graph, 4.8
+// TFLOP/s): a decode step of 32 sequences of 28 / 4 heads and 1280 to 2047 slots, 112 MB, 23.7 us in a graph, 4.7
 // TB/s: the memory. 4096 tokens of 32 / 8 heads behind 4096, 412 GFLOP, 421 to 474 us by card, 870 to 980
 // TFLOP/s: of a wave's time a third is matrix instructions and as much the exponentials with their maxima, sums
 // and roundings, which the other wave of its SIMD covers in part; the rest is issuing loads and scalar code.
@@ -182,6 +182,16 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {  // to nearest
   return __builtin_bit_cast(uint32_t, bf16x2{(__bf16)a, (__bf16)b});
 }
 
+// Two values that are not negative as bfloat16, each the largest below it, and what is left, rounded: the sum of
+// both is within 2^-16 of the value, and neither is 0 unless the value is (0 x inf would be NaN).
+struct TwoTerms {
+  uint32_t most, rest;
+};
+__device__ __forceinline__ TwoTerms split_bf16(float a, float b) {
+  const uint32_t x = bf16_below(a), y = bf16_below(b);
+  return {x >> 16 | y, pack_bf16(a - __uint_as_float(x), b - __uint_as_float(y))};
+}
+
 __device__ __forceinline__ bool odd_bits(uint32_t x, bool f32) {  // an infinity or NaN in a word
   return f32 ? (x & 0x7f800000u) == 0x7f800000u
              : (x & 0x7f800000u) == 0x7f800000u || (x & 0x7f80u) == 0x7f80u;
@@ -291,6 +301,13 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
   using C = Team<T, D, KW, DV, RW>;
   static_assert(RW == 32 || (C::kF32 && KW > 1), "16 rows: float32, few rows");
   constexpr bool F32 = C::kF32;
+  // How bfloat16 weights enter the product with V. Few rows: as two terms, within 2^-16, as in lg_decode_attend; memory
+  // bounds these steps (32 sequences of 28 / 4 heads above: 23.7 us, 22.8 with one term; 64 sequences of 32 / 8 heads
+  // and 1024 slots 40.6 and 39.7). Chunks of more than 32 rows: rounded once, since their matrix instructions bound them:
+  // with two terms 4096 tokens behind 4096 take 577 us (429), at head_dim 64 372 (280), 8 x 128 tokens of a window of
+  // 1024 51 (43). An output then lies within 2^-8 sum alpha |v|; against 64 bits, over all outputs of a mixed
+  // step, 1.71e-3 where the outputs' own rounding is 1.67e-3.
+  constexpr bool kTwoTerms = !F32 && KW > 1;
   constexpr int NK = C::kKeys, NB = NK / 32, ND = DV / RW, RB = C::kRowBytes, RBV = C::kRowBytesV;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int part = lane / RW, col = lane % RW;
@@ -587,9 +604,18 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
     } else {
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        u32x4_t p;  // the weights as bfloat16: the matrix product's type
+        u32x4_t p, rest;  // the weights as bfloat16, the matrix product's type
 #pragma unroll
-        for (int e = 0; e < 4; ++e) p[e] = pack_bf16(P[8 * s + 2 * e], P[8 * s + 2 * e + 1]);
+        for (int e = 0; e < 4; ++e) {
+          const float x = P[8 * s + 2 * e], y = P[8 * s + 2 * e + 1];
+          if constexpr (kTwoTerms) {
+            const TwoTerms two = split_bf16(x, y);
+            p[e] = two.most;
+            rest[e] = two.rest;
+          } else {
+            p[e] = pack_bf16(x, y);
+          }
+        }
         // a 16-lane group reads 4 keys x 16 values and gets them transposed: lane = value
 #pragma unroll
         for (int d = 0; d < ND; ++d) {
@@ -601,6 +627,9 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
           const u32x4_t z = {x[0], x[1], y[0], y[1]};
           O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, z), __builtin_bit_cast(bf16x8, p),
                                                          O[d], 0, 0, 0);
+          if constexpr (kTwoTerms)
+            O[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, z),
+                                                           __builtin_bit_cast(bf16x8, rest), O[d], 0, 0, 0);
         }
       }
     }
