@@ -531,7 +531,8 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
   auto suffix_of = [&]() __attribute__((always_inline)) {
     if (a.suffix == nullptr && a.conf == nullptr) return (int)kNone;
     const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
-    return p_last <= suf_lo ? (int)kNone : p_first > suf_hi ? (int)kAll : (int)kSome;
+    // kHidden in front says nothing about the slots behind it
+    return p_last <= suf_lo ? (int)kNone : p_first > suf_hi && p_first != kHidden ? (int)kAll : (int)kSome;
   };
   auto add_suffix = [&](const Weights& P, int nb) __attribute__((always_inline)) {
 #pragma unroll
