@@ -1116,6 +1116,10 @@ constexpr long kHalvesReach = 2560, kHalvesPairs = 64;
 // of 1000 slots 103 / 76 / 65.5 / 48.6 (the capacity is all the host knows).
 constexpr long kMaxSplitSlotsPaged = 32768;
 
+// Rows (of a token and a query head) that a launch joins at most: its 256 threads a workgroup must stay below the 2^32 of
+// a grid, 8 rows a workgroup at head_dim 128. A larger step has a million workgroups and is not split.
+constexpr long kMaxJoinRows = (1l << 27) - 8;
+
 // reach: slots that a token may see, by the capacity and the window.
 static PagedPlan paged_plan(const lg_paged_layer& l, const lg_page_map& m, long total, long max_chunk, long reach) {
   const long G = l.n_q_heads / l.n_kv_heads;
@@ -1146,6 +1150,7 @@ static PagedPlan paged_plan(const lg_paged_layer& l, const lg_page_map& m, long 
     p.halves = 2;
   }
   p.ns = (int)std::max({ns, least, 1l});
+  if (total * l.n_q_heads > kMaxJoinRows) p.ns = 1;
   return p;
 }
 
