@@ -218,9 +218,13 @@ struct ForkArgs {
 constexpr int kForkThreads = 256;
 constexpr int kForkSlots = 1024;  // of capacity for a workgroup ...
 constexpr int kForkSpread = 64;   // ... up to this many a sequence
-// Slots of capacity of all sequences up to which one workgroup takes both steps: a call 4.7 us for 4 x 256 slots and
-// 6.0 for 8 x 1024, in two launches 7.5 and 7.8 (4 us of it the host's second launch); in a graph 3.7 / 6.3 against 5.2 /
-// 6.3, and behind from there on (8.7 against 6.3 for 8 x 2048).
+// One workgroup takes both steps of small maps: up to kForkSmallBatch sequences, of which it works on four at once, each
+// round a chain of dependent reads, and kForkSmall slots of capacity in all. Sequences x slots in a graph / a call, in two
+// launches behind the stroke (a call's second launch costs the host 4 us):
+//   4 x 256 3.5 / 4.7 us | 5.4 / 7.2    8 x 512 5.3 / 5.0 | 5.5 / 7.0    8 x 1024 6.9 / 6.5 | 6.3 / 7.1
+//   8 x 2048 9.2 / 8.9 | 6.2 / 7.3      16 x 256 8.8 / 8.4 | 5.5 / 7.1   32 x 256 15.4 / 15.1 | 5.7 / 7.0
+//   64 x 128 32.6 / 32.4 | 5.6 / 7.0    512 x 16 281 / 280 | 5.8 / 7.3
+constexpr int kForkSmallBatch = 8;
 constexpr long kForkSmall = 8192;
 
 __device__ __forceinline__ bool fork_changes(const ForkArgs& a, int b, int* parent) {
@@ -538,7 +542,7 @@ hipError_t launch_fork(const lg_page_map& map, const int32_t* parent, void* ws, 
   a.map = map_args(map);
   a.ws = page_ws(map, ws);
   a.parent = parent;
-  if ((long)map.batch * a.map.cap <= kForkSmall) {
+  if (map.batch <= kForkSmallBatch && (long)map.batch * a.map.cap <= kForkSmall) {
     hipLaunchKernelGGL(fork_small, dim3(1), dim3(kMapThreads), 0, st, a);
     return hipGetLastError();
   }
