@@ -20,6 +20,19 @@
  *
  * lg_page_fork makes sequences continue others (beams, samples of one prompt) or end.
  *
+ * Beside the guard. What belongs to a sequence and is not in the map is the caller's: its row of
+ * lg_guard_state, of the token ring, of t, t0, budget, suffix_w and conf.
+ *   - lg_page_fork leaves those rows as they are. A sequence that continues another takes the parent's with
+ *     it (row b <- row parent[b]); one that begins anew starts from a zeroed state.
+ *   - lg_detect_loop takes a step for every sequence of its batch. For one that brought no token in
+ *     this step that is one step too many: conf is 0, so its streak ends, and stall and rep count the same
+ *     tail once more. Copy its row of the state before step 4 and back behind it, and zero its decision
+ *     before step 5 (the length alone then decides about a prune).
+ *   - The last token of each piece of a prompt raises conf too: zero conf behind the prompt where it
+ *     shall not count.
+ *   - LG_POLICY_H2O is not available: lg_paged_attend forms no acc, and step 5 without layers takes all
+ *     scores as 0, which keeps the newest slots alone.
+ *
  * Conventions are those of lg.h: caller-owned device memory, no allocation, no synchronisation, host
  * checks before anything is enqueued, device-side values clamped into the buffers. Calls keep no
  * state but in the arrays they are given; a workspace is written before it is read in every call, so
@@ -28,12 +41,13 @@
  *
  * The map. `table[b][c]` is the page of slots [c page_size, (c + 1) page_size) of sequence b, or -1.
  * `ref[p]` counts the table entries that name page p: 0 is a free page. Live slots 0..len[b]-1 hold
- * strictly increasing positions, as in lg.h, below 2^31 - 1; the columns below
- * ceil(len[b] / page_size) name pages and the others are -1. An empty map is table = -1, len = 0, ref = 0. All calls here keep this, and
- * ask for it: other values (a page number outside the pool, say) give unspecified results for the
- * sequences that hold them, without any access outside the buffers. A caller may hold pages back
- * by counting them once more in ref. Pages are taken in ascending order of their number, for the
- * sequences in ascending order, so every result is a function of the inputs alone.
+ * strictly increasing positions, as in lg.h, from 0 up and below 2^31 - 1; the columns below
+ * ceil(len[b] / page_size) name pages and the others are -1. An empty map is table = -1, len = 0,
+ * ref = 0. All calls here keep this, and ask for it: other values (a page number outside the pool,
+ * say) give unspecified results for the sequences that hold them, without any access outside the
+ * buffers. A caller may hold pages back by counting them once more in ref. Pages are taken in
+ * ascending order of their number, for the sequences in ascending order, so every result is a
+ * function of the inputs alone.
  *
  * When pages run out. A call that takes pages meets the sequences' needs in order, up to the first
  * that what is free does not cover; that sequence and every later one that needs any page is
@@ -78,7 +92,8 @@ size_t lg_page_workspace(const lg_page_map* map);
  * A last page that holds live slots, will take new ones and is shared (ref > 1) is replaced by a page
  * of its own with its live rows copied, in every layer given; the shared one loses this reference.
  * A sequence is refused when pages run out (see above) or n exceeds its columns: base[b] = -1, and
- * the calls that take base leave its rows alone. With n = 0, base[b] = len[b].
+ * the calls that take base leave its rows alone. With n = 0, base[b] = len[b]. The first new position,
+ * t[b] - n + 1, is the caller's to have at 0 or above and behind the last live one (see the map).
  *   layers       host array of n_layers views (0: the map alone; then the caller copies rows of pages).
  *                All have the same sizes and type (LG_ERR_SHAPE), and no pages in common.
  *   q_start      [batch + 1] int32, ascending.
@@ -149,7 +164,7 @@ lg_status lg_rope_frequencies(const lg_rope_params* p, float* inv_freq, float* s
  *                is not), and overlaps none of q, k, v in any other way.
  *   inv_freq     [rot_dim / 2] float32 device array; may be NULL with rot_dim 0 (append alone).
  *   rot_dim      even, 0 <= rot_dim <= head_dim (LG_ERR_PARAM).
- *   total        rows of q, k and v; 0 enqueues nothing. */
+ *   total        rows of q, k and v, below 2^23 (LG_ERR_SHAPE); 0 enqueues nothing. */
 lg_status lg_rope_append(const lg_paged_layer* layer, const lg_page_map* map, const void* q,
                          int64_t q_stride, const void* k, int64_t k_stride, const void* v,
                          int64_t v_stride, const float* inv_freq, int32_t rot_dim,
@@ -177,7 +192,9 @@ size_t lg_paged_attend_workspace(const lg_paged_layer* layer, const lg_page_map*
  *   q, out       [total][n_q_heads][head_dim] dtype, 16-byte aligned; out may not overlap q (LG_ERR_PARAM
  *                for out = q).
  *   max_chunk    the largest number of tokens of a sequence; one that brings more is treated as
- *                refused. total, max_chunk: >= 0; 0 total enqueues nothing.
+ *                refused. total, max_chunk: >= 0; 0 total enqueues nothing. total * n_q_heads < 2^31, and the
+ *                workgroups (one for every 128 query rows of a KV head, one for every sequence and KV head,
+ *                times the splits) < 2^23 (LG_ERR_SHAPE).
  *   window, n_sink  >= 0 (LG_ERR_PARAM).
  *   suffix_w     [batch] int32 >= 0, or NULL: then suffix_mass and conf must be NULL too. p - suffix_w[b]
  *                and p - window saturate.
