@@ -84,7 +84,7 @@ struct PagedAttendArgs {
   float scale_log2;
 };
 
-// Sizes of the team that shares a tile: the workgroup (KW = 1) or a wave (KW = 4, 8).
+// Sizes of the team that shares a tile: the workgroup (KW = 1) or a wave (KW = 2, 4, 8).
 //
 // A row of K or V in LDS is its 16-byte pieces in the order piece ^ f(row): the 16 rows whose pieces one read
 // of K takes, and the 4 rows (of 64 bytes) that a transposed read of V takes, then lie in different banks,
@@ -271,7 +271,9 @@ __device__ __forceinline__ void job_tiles(const PagedAttendArgs& a, Job& job, in
 // that decode with a window of 4096 over a history thinned out four to one: 58 us, 100 without.
 template <int NK>
 __device__ __forceinline__ bool skip_hidden(const PagedAttendArgs& a, Job& job, const int32_t* pos) {
-  if (job.tile0 == 0) return false;  // no window, or all of the cache within it
+  // No window, or one of at least as many positions as the cache holds slots: nothing is looked for, and slots that
+  // holes in the positions put out of such a window are compared and masked.
+  if (job.tile0 == 0) return false;
   const int slot = job.base + job.row0 / a.G, lane = threadIdx.x & 63;
   const int w = (int)max((long long)pos[slot] - a.window, (long long)INT32_MIN);
   int lo = job.tile0, hi = slot / NK;  // the tile of the token's own slot is seen
