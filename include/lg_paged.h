@@ -121,7 +121,8 @@ lg_status lg_page_fork(const lg_page_map* map, const int32_t* parent, void* work
  *   moved [batch] int32 output: 1 moved, 0 not flagged, -1 refused (the pages for its replacements
  *         are not there). A refused sequence's table, pages and references are as before while its
  *         pos and len say what they will hold: free pages and repeat the call, with new_len = -1 for
- *         the sequences that have moved, or end it (lg_page_fork).
+ *         the sequences that have moved, or end it (lg_page_fork), before it
+ *         attends again: until then its positions name other rows than its pages hold.
  *   keep_idx [batch][max_pages * page_size], new_len [batch] int32. */
 lg_status lg_page_compact(const lg_page_map* map, int32_t n_layers, const lg_paged_layer* layers,
                           const int32_t* keep_idx, const int32_t* new_len, int32_t* moved,

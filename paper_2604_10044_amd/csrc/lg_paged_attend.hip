@@ -305,7 +305,7 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
   constexpr bool F32 = C::kF32;
   // How bfloat16 weights enter the product with V. Few rows: as two terms, within 2^-16, as in lg_decode_attend; memory
   // bounds these steps (32 sequences of 28 / 4 heads above: 23.7 us, 22.8 with one term; 64 sequences of 32 / 8 heads
-  // and 1024 slots 40.6 and 39.7). Chunks of more than 32 rows: rounded once, since their matrix instructions bound them:
+  // and 1024 slots 40.6 and 39.7; most where few tiles a wave leave the chain to show: 16 of 28 / 4 and 2048 18.7 and 17.1). Chunks of more than 32 rows: rounded once, since their matrix instructions bound them:
   // with two terms 4096 tokens behind 4096 take 577 us (429), at head_dim 64 372 (280), 8 x 128 tokens of a window of
   // 1024 51 (43). An output then lies within 2^-8 sum alpha |v|; against 64 bits, over all outputs of a mixed
   // step, 1.71e-3 where the outputs' own rounding is 1.67e-3.
@@ -1109,8 +1109,9 @@ struct PagedPlan {
 constexpr long kFewTarget = 256;
 // Three or four splits (64 pairs of a sequence and a KV head on) take more than two halves without a join up to this many
 // slots (bfloat16, head_dim 128: in float32 the scores, which both halves form, bound it). Decode steps of 16 / 20
-// sequences, 28 / 4 heads, 2048 slots 17.3 / 18.2 us, split 18.5 / 20.9; 16 of 4096 slots 26.5, split 25.4. With fewer pairs
-// the two are within half a microsecond at 1024 slots and splits ahead behind that.
+// sequences, 28 / 4 heads, 1024 slots 12.6 / 13.0 us, split 12.5 / 13.9; 2048 slots 19.1 / 19.5, split 18.3 / 21.0; 3008 slots
+// 23.5 / 25.6, split 22.6 / 25.5; 4096 slots 29.5 / 31.0, split 25.5 / 30.3. With fewer pairs the two are within half a
+// microsecond at 1024 slots and splits ahead behind that.
 constexpr long kHalvesReach = 2560, kHalvesPairs = 64;
 // Slots of a split at most, whatever the number of workgroups: what one long sequence among many short ones
 // may hold up the launch by. Decode steps of 32 / 8 heads over 65536 slots of capacity, at 8192 / 16384 / 32768

@@ -5,7 +5,8 @@
 // rot_dim / 2 angles are formed once in LDS for all heads (one thread each), and the threads walk the
 // token's heads in 16-byte pieces. Every value is read once and written once, so memory bounds the
 // kernel at long chunks and launch latency at one token a sequence. Measured: 403 MB (two bf16 prompts
-// of 8192 tokens, 32 + 8 heads of 128) in 70.5 us, 5.7 TB/s; one token of 32 sequences in 3.8 us.
+// of 8192 tokens, 32 + 8 heads of 128) in 70.5 us, 5.7 TB/s; one token of 32 sequences in 3.8 us. Rotated parts that
+// are no whole pieces (kRopeAny) go value by value: the two prompts with 100 rotated values 168 us, 177 interleaved.
 //
 // An angle p * f is reduced in double to a fraction of a turn in [-1/2, 1/2] (positions reach 2^30: a
 // float32 product would keep no digit of the fraction), and only the fraction is rounded to float32.
