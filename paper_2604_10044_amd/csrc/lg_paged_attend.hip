@@ -305,10 +305,11 @@ __device__ __forceinline__ void paged_body(const PagedAttendArgs& a, Job job, ch
   constexpr bool F32 = C::kF32;
   // How bfloat16 weights enter the product with V. Few rows: as two terms, within 2^-16, as in lg_decode_attend; memory
   // bounds these steps (32 sequences of 28 / 4 heads above: 23.7 us, 22.8 with one term; 64 sequences of 32 / 8 heads
-  // and 1024 slots 40.6 and 39.7; most where few tiles a wave leave the chain to show: 16 of 28 / 4 and 2048 18.7 and 17.1). Chunks of more than 32 rows: rounded once, since their matrix instructions bound them:
-  // with two terms 4096 tokens behind 4096 take 577 us (429), at head_dim 64 372 (280), 8 x 128 tokens of a window of
-  // 1024 51 (43). An output then lies within 2^-8 sum alpha |v|; against 64 bits, over all outputs of a mixed
-  // step, 1.71e-3 where the outputs' own rounding is 1.67e-3.
+  // and 1024 slots 40.6 and 39.7; most where few tiles a wave leave the chain to show: 16 of 28 / 4 and 2048 slots 18.7
+  // and 17.1). Chunks of more than 32 rows: rounded once, since their matrix instructions bound them: with two terms 4096
+  // tokens behind 4096 take 577 us (429), at head_dim 64 372 (280), 8 x 128 tokens of a window of 1024 51 (43). An
+  // output then lies within 2^-8 sum alpha |v|; against 64 bits, over all outputs of a mixed step, 1.71e-3 where the
+  // outputs' own rounding is 1.67e-3.
   constexpr bool kTwoTerms = !F32 && KW > 1;
   constexpr int NK = C::kKeys, NB = NK / 32, ND = DV / RW, RB = C::kRowBytes, RBV = C::kRowBytesV;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
