@@ -63,7 +63,8 @@ typedef enum {
   LG_ERR_TOO_LARGE = 8    /* lg_decode_attend_noalloc: the layer needs more than its scratch */
 } lg_status;
 
-typedef enum { LG_F32 = 0, LG_BF16 = 1 } lg_dtype;
+/* LG_FP4: 4-bit pages (lg_fp4.h), which no call of this header takes. */
+typedef enum { LG_F32 = 0, LG_BF16 = 1, LG_FP4 = 4 } lg_dtype;
 
 /* One layer's KV cache (Sec. 3.1: per-head keys/values of the accessible set S_t, |S_t| <= B).
  *   k, v : [batch][n_kv_heads][cap][head_dim] of dtype, row-major; slot j of sequence b holds

@@ -56,4 +56,13 @@ __device__ __forceinline__ int seq_of_row(const int32_t* q_start, int B, int r) 
   return b;
 }
 
+// 4-bit layers (lg_fp4.h): bytes of a row's values, of its exponents, and of the block of a page and a head.
+constexpr int kFp4Group = 32;  // values of one exponent
+__host__ __device__ __forceinline__ constexpr int fp4_row(int D) { return D / 2; }
+__host__ __device__ __forceinline__ constexpr int fp4_exps(int D) { return D / kFp4Group; }
+__host__ __device__ __forceinline__ size_t fp4_block(int D, int shift) { return (size_t)(fp4_row(D) + fp4_exps(D)) << shift; }
+
+// The unit 2^(x - 127) of an exponent byte as the conversion instructions take it: NaN above 252.
+__device__ __forceinline__ float fp4_unit(uint32_t x) { return __uint_as_float((x > 252 ? 255u : x) << 23); }
+
 }  // namespace lg

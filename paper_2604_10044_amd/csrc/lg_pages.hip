@@ -182,7 +182,9 @@ struct LayerPtrs {
 struct CopyArgs {
   LayerPtrs layer;
   PageWs ws;
-  int32_t n_layers, Hkv, shift, row_bytes;
+  int32_t n_layers, Hkv;
+  int32_t row_bytes, exp_bytes;  // exp_bytes: of a 4-bit row's exponents, which lie behind the page's rows (else 0)
+  int32_t shift;
 };
 
 constexpr int kCopyThreads = 256;
@@ -196,15 +198,16 @@ __global__ __launch_bounds__(kCopyThreads) void copy_rows(CopyArgs a) {
   const int copies = a.ws.count[0];
   const int per = 2 * a.n_layers * a.Hkv;
   const long long items = (long long)copies * per;
-  const size_t head = (size_t)a.row_bytes << a.shift;
+  const size_t head = (size_t)(a.row_bytes + a.exp_bytes) << a.shift, exps = (size_t)a.row_bytes << a.shift;
   for (long long it = blockIdx.x; it < items; it += gridDim.x) {
     const int b = a.ws.list[it / per], x = (int)(it % per);
     const int h = x % a.Hkv, l = x / a.Hkv % a.n_layers;
     char* pages = (char*)(x < a.n_layers * a.Hkv ? a.layer.k[l] : a.layer.v[l]);
     const u32x4_t* src = (const u32x4_t*)(pages + ((size_t)a.ws.src[b] * a.Hkv + h) * head);
     u32x4_t* dst = (u32x4_t*)(pages + ((size_t)a.ws.dst[b] * a.Hkv + h) * head);
-    const int n = a.ws.first[b] * (a.row_bytes / 16);
+    const int n = a.ws.first[b] * (a.row_bytes / 16), ne = a.ws.first[b] * a.exp_bytes;
     for (int i = threadIdx.x; i < n; i += kCopyThreads) dst[i] = src[i];
+    for (int i = threadIdx.x; i < ne; i += kCopyThreads) ((uint8_t*)dst)[exps + i] = ((const uint8_t*)src)[exps + i];
   }
 }
 
@@ -398,7 +401,8 @@ struct MoveArgs {
   MapArgs map;
   const int32_t *keep_idx, *new_len;
   int32_t n_layers, Hkv, row_bytes;
-  int32_t n_col;  // 128-byte columns of a K row and a V row together
+  int32_t n_col;    // columns of a K row and a V row together: 128 bytes each, in 4 bits a whole row
+  int32_t head_dim;
 };
 
 // Threads x rows in flight a thread, for one sequence of 28 layers (166 MB, read and written) / eight of 16 (3.0 GB),
@@ -408,8 +412,6 @@ constexpr int kMoveThreads = 1024;
 constexpr int kMoveUnroll = 4;  // rows in flight per thread
 constexpr int kColBytes = 128;
 constexpr int kColLanes = kColBytes / 16;
-constexpr int kPassRows = kMoveThreads / kColLanes;
-constexpr int kRowsPerPass = kPassRows * kMoveUnroll;
 constexpr int kSegmentRows = 2048;  // rows whose places are looked up at once
 constexpr int kMoveWorkgroups = 1024;
 constexpr uint32_t kStays = 0xffffffffu;
@@ -421,36 +423,62 @@ constexpr uint32_t kStays = 0xffffffffu;
 // ends), so a segment's rows look them up together and the passes find them in LDS, as slots of the pool (page x
 // page_size + row: below 2^32, since a slot has 128 bytes at least).
 // Memory bounds it: 3.0 GB in 534 us, 5.6 TB/s, where a copy of 1 GiB runs at 5.2.
+//
+// 4-bit rows (L = 4 or 2 lanes of 16 bytes, in place of 8): an item is the whole row with its exponents, a byte a lane.
+template <int L>
 struct Moves {
   u32x4_t x[kMoveUnroll];
+  uint8_t e[L < kColLanes ? kMoveUnroll : 1];
 };
 
 __device__ __forceinline__ size_t pool_row(const MapArgs& m, uint32_t slot, int Hkv, int h) {
   return (((size_t)(slot >> m.shift) * Hkv + h) << m.shift) + (slot & ((1u << m.shift) - 1));
 }
 
-__device__ __forceinline__ void move_load(const MoveArgs& a, Moves& v, int r0, int n, int h, const uint32_t* src,
-                                          const char* col) {
-#pragma unroll
-  for (int u = 0; u < kMoveUnroll; ++u) {
-    const int r = r0 + u * kPassRows + (int)threadIdx.x / kColLanes;
-    const uint32_t s = r < n ? src[r] : kStays;
-    if (s != kStays)
-      v.x[u] = __builtin_nontemporal_load((const u32x4_t*)(col + pool_row(a.map, s, a.Hkv, h) * a.row_bytes));
+// Where the lane's 16 bytes of a slot's row lie, and its exponent byte behind the page's rows.
+template <int L>
+__device__ __forceinline__ char* move_at(const MoveArgs& a, uint32_t slot, int h, char* col, char** exps) {
+  if constexpr (L == kColLanes) {
+    return col + pool_row(a.map, slot, a.Hkv, h) * a.row_bytes;
+  } else {
+    const uint32_t row = slot & ((1u << a.map.shift) - 1);
+    char* block = col + ((size_t)(slot >> a.map.shift) * a.Hkv + h) * fp4_block(a.head_dim, a.map.shift);
+    *exps = block + ((size_t)(16 * L) << a.map.shift) + row * L + threadIdx.x % L;
+    return block + row * (16 * L) + 16 * (threadIdx.x % L);
   }
 }
 
-__device__ __forceinline__ void move_store(const MoveArgs& a, const Moves& v, int r0, int n, int h, const uint32_t* src,
+template <int L>
+__device__ __forceinline__ void move_load(const MoveArgs& a, Moves<L>& v, int r0, int n, int h, const uint32_t* src, char* col) {
+#pragma unroll
+  for (int u = 0; u < kMoveUnroll; ++u) {
+    const int r = r0 + u * (kMoveThreads / L) + (int)threadIdx.x / L;
+    const uint32_t s = r < n ? src[r] : kStays;
+    if (s != kStays) {
+      char* e = nullptr;
+      v.x[u] = __builtin_nontemporal_load((const u32x4_t*)move_at<L>(a, s, h, col, &e));
+      if constexpr (L < kColLanes) v.e[u] = *(const uint8_t*)e;
+    }
+  }
+}
+
+template <int L>
+__device__ __forceinline__ void move_store(const MoveArgs& a, const Moves<L>& v, int r0, int n, int h, const uint32_t* src,
                                            const uint32_t* dst, char* col) {
 #pragma unroll
   for (int u = 0; u < kMoveUnroll; ++u) {
-    const int r = r0 + u * kPassRows + (int)threadIdx.x / kColLanes;
-    if (r < n && src[r] != kStays)
-      __builtin_nontemporal_store(v.x[u], (u32x4_t*)(col + pool_row(a.map, dst[r], a.Hkv, h) * a.row_bytes));
+    const int r = r0 + u * (kMoveThreads / L) + (int)threadIdx.x / L;
+    if (r < n && src[r] != kStays) {
+      char* e = nullptr;
+      __builtin_nontemporal_store(v.x[u], (u32x4_t*)move_at<L>(a, dst[r], h, col, &e));
+      if constexpr (L < kColLanes) *(uint8_t*)e = v.e[u];
+    }
   }
 }
 
+template <int L>
 __global__ __launch_bounds__(kMoveThreads) void move_rows(MoveArgs a) {
+  constexpr int kRowsPerPass = kMoveThreads / L * kMoveUnroll;
   __shared__ uint32_t src[kSegmentRows], dst[kSegmentRows];
   const MapArgs& m = a.map;
   const int per = a.n_layers * a.Hkv * a.n_col, mask = (1 << m.shift) - 1;
@@ -460,8 +488,8 @@ __global__ __launch_bounds__(kMoveThreads) void move_rows(MoveArgs a) {
     const int b = a.ws.list[it / per], x = (int)(it % per);
     const int l = x % a.n_layers, y = x / a.n_layers;
     const int c = y % a.n_col, h = y / a.n_col, half = a.n_col / 2;
-    char* col = (char*)(c < half ? a.layer.k[l] : a.layer.v[l]) + (c % half) * kColBytes +
-                16 * (threadIdx.x % kColLanes);
+    char* col = (char*)(c < half ? a.layer.k[l] : a.layer.v[l]);
+    if constexpr (L == kColLanes) col += (c % half) * kColBytes + 16 * (threadIdx.x % kColLanes);
     const int nl = min(a.new_len[b], m.cap);
     const int32_t* keep = a.keep_idx + (size_t)b * m.cap;
     const int32_t *from = a.ws.table + (size_t)b * m.P, *to = m.table + (size_t)b * m.P;
@@ -486,7 +514,7 @@ __global__ __launch_bounds__(kMoveThreads) void move_rows(MoveArgs a) {
         }
         __syncthreads();
       }
-      Moves cur, nxt;
+      Moves<L> cur, nxt;
       move_load(a, cur, 0, n, h, src, col);
       for (int r0 = 0; r0 < n; r0 += kRowsPerPass) {
         __syncthreads();  // every thread holds this pass's rows
@@ -510,7 +538,9 @@ static void layer_ptrs(LayerPtrs* p, const lg_paged_layer* layers, int n) {
   }
 }
 
-static int row_bytes_of(const lg_paged_layer& l) { return l.head_dim * (l.dtype == LG_BF16 ? 2 : 4); }
+static int row_bytes_of(const lg_paged_layer& l) {
+  return l.dtype == LG_FP4 ? fp4_row(l.head_dim) : l.head_dim * (l.dtype == LG_BF16 ? 2 : 4);
+}
 
 hipError_t launch_reserve(const lg_page_map& map, int n_layers, const lg_paged_layer* layers,
                           const int32_t* q_start, const int32_t* t, int32_t* base, void* ws,
@@ -531,6 +561,7 @@ hipError_t launch_reserve(const lg_page_map& map, int n_layers, const lg_paged_l
     c.Hkv = layers[0].n_kv_heads;
     c.shift = a.map.shift;
     c.row_bytes = row_bytes_of(layers[0]);
+    c.exp_bytes = layers[0].dtype == LG_FP4 ? fp4_exps(layers[0].head_dim) : 0;
     const long long items = 2ll * c.n_layers * c.Hkv * map.batch;
     hipLaunchKernelGGL(copy_rows, dim3((unsigned)min(items, (long long)kCopyWorkgroups)),
                        dim3(kCopyThreads), 0, st, c);
@@ -576,11 +607,13 @@ hipError_t launch_page_compact(const lg_page_map& map, int n_layers, const lg_pa
     c.keep_idx = keep_idx;
     c.new_len = new_len;
     c.Hkv = layers[0].n_kv_heads;
+    c.head_dim = layers[0].head_dim;
+    const bool fp4 = layers[0].dtype == LG_FP4;
     c.row_bytes = row_bytes_of(layers[0]);
-    c.n_col = 2 * c.row_bytes / kColBytes;
+    c.n_col = fp4 ? 2 : 2 * c.row_bytes / kColBytes;
     const long long items = (long long)c.n_layers * c.Hkv * c.n_col * map.batch;
-    hipLaunchKernelGGL(move_rows, dim3((unsigned)min(items, (long long)kMoveWorkgroups)),
-                       dim3(kMoveThreads), 0, st, c);
+    const auto move = !fp4 ? move_rows<kColLanes> : c.head_dim == 128 ? move_rows<4> : move_rows<2>;
+    hipLaunchKernelGGL(move, dim3((unsigned)min(items, (long long)kMoveWorkgroups)), dim3(kMoveThreads), 0, st, c);
     e = hipGetLastError();
   }
   return e;

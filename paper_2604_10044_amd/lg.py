@@ -1,4 +1,4 @@
-"""Python binding of liblg (the C ABI in include/lg.h and include/lg_paged.h): argument marshalling only.
+"""Python binding of liblg (the C ABI in include/lg.h, lg_paged.h and lg_fp4.h): argument marshalling only.
 
 Every function here has the name of the C entry point it calls and takes torch tensors (device
 memory) in place of raw pointers; those of the paged cache check the tensors' types, sizes, layout and
@@ -21,7 +21,7 @@ if not os.path.exists(LIB_PATH):
                       "python -m paper_2604_10044_amd.build)")
 _lib = ctypes.CDLL(LIB_PATH)
 
-LG_F32, LG_BF16 = 0, 1
+LG_F32, LG_BF16, LG_FP4 = 0, 1, 4
 LG_ATTEND_STATUS_WAIT, LG_ATTEND_STATUS_WORKSPACE = 1, 2
 # test hooks (include/lg_testing.h)
 FORM_AUTO, FORM_PORTABLE, FORM_MERGE, FORM_ONE_LAUNCH = 0, 1, 2, 3
@@ -29,6 +29,7 @@ TEST_FORCE_HANDOVER, TEST_NO_WAIT, TEST_WHOLE_DIMS = 1, 2, 4
 LG_MODE_FULL, LG_MODE_ALWAYS_ON, LG_MODE_P1_ONLY = 0, 1, 2
 LG_POLICY_LOOPGUARD, LG_POLICY_H2O, LG_POLICY_STREAMING = 0, 1, 2
 LG_ROPE_PLAIN, LG_ROPE_LINEAR, LG_ROPE_BASE, LG_ROPE_RAMP, LG_ROPE_BANDS = 0, 1, 2, 3, 4
+LG_AXES_BLOCKS, LG_AXES_TURNS = 0, 1
 STATUS = {0: "LG_OK", 1: "LG_ERR_NULL", 2: "LG_ERR_SHAPE", 3: "LG_ERR_UNSUPPORTED",
           4: "LG_ERR_PARAM", 5: "LG_ERR_WORKSPACE", 6: "LG_ERR_HIP", 7: "LG_ERR_ALIGN",
           8: "LG_ERR_TOO_LARGE"}
@@ -77,7 +78,7 @@ class PageMap(ctypes.Structure):
 
 
 class PagedLayer(ctypes.Structure):
-    """lg_paged_layer; made by paged_layer(), which keeps the tensors alive in `tensors`."""
+    """lg_paged_layer; made by paged_layer() or paged_layer_fp4(), which keep the tensors alive in `tensors`."""
     _fields_ = [("n_pages", ctypes.c_int32), ("page_size", ctypes.c_int32),
                 ("n_q_heads", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
                 ("head_dim", ctypes.c_int32), ("dtype", ctypes.c_int), ("k", ctypes.c_void_p),
@@ -143,6 +144,18 @@ _lib.lg_paged_attend_workspace.argtypes = [_PP, _MP, _i32, _i32]
 _lib.lg_paged_attend.restype = ctypes.c_int
 _lib.lg_paged_attend.argtypes = [_PP, _MP, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp, _sz,
                                  _vp]
+_lib.lg_rope_axes.restype = ctypes.c_int
+_lib.lg_rope_axes.argtypes = [_i32, _vp, _i32, _vp]
+_lib.lg_rope_append_axes.restype = ctypes.c_int
+_lib.lg_rope_append_axes.argtypes = [_PP, _MP, ctypes.c_int, _vp, _i64, _vp, _i64, _vp, _i64, _vp, _i32, _i32, ctypes.c_float,
+                                     _vp, _vp, _i64, _i32, _vp, _vp, _vp, _i32, _vp]
+_lib.lg_page_unpack_fp4.restype = ctypes.c_int
+_lib.lg_page_unpack_fp4.argtypes = [_PP, _MP, ctypes.c_int, _vp, _vp, _vp, _vp, _i32, _vp]
+_lib.lg_paged_attend_fp4_workspace.restype = _sz
+_lib.lg_paged_attend_fp4_workspace.argtypes = [_PP, _MP, ctypes.c_int, _i32, _i32]
+_lib.lg_paged_attend_fp4.restype = ctypes.c_int
+_lib.lg_paged_attend_fp4.argtypes = [_PP, _MP, ctypes.c_int, _vp, _vp, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _vp, _vp, _vp, _vp,
+                                     _sz, _vp]
 _lib.lg_copy_bandwidth.restype = ctypes.c_int
 _lib.lg_copy_bandwidth.argtypes = [_vp, _vp, _sz, _vp]
 
@@ -455,6 +468,121 @@ def lg_paged_attend(layer: PagedLayer, m: PageMap, q, out, q_start, base, max_ch
         None if suffix_mass is None else _need(suffix_mass, f32, n, dev, "suffix_mass"),
         None if conf is None else _need(conf, f32, B, dev, "conf"), ws, size, stream),
         "lg_paged_attend")
+
+
+# ------------------------------------------------------------------------------------------------
+# 4-bit pages and rotary positions with several axes (include/lg_fp4.h).
+# ------------------------------------------------------------------------------------------------
+_NUMBER = {torch.float32: LG_F32, torch.bfloat16: LG_BF16}
+
+
+def _number(dtype, what):
+    """The lg_dtype of a call's own tensors."""
+    if dtype not in _NUMBER:
+        raise LGError("%s: needs float32 or bfloat16 tensors, got %s" % (what, dtype))
+    return _NUMBER[dtype]
+
+
+def fp4_page_bytes(page_size: int, head_dim: int) -> int:
+    """Bytes of one head in a page of a 4-bit layer: its rows, and behind them the exponents."""
+    return page_size * (head_dim // 2 + head_dim // 32)
+
+
+def paged_layer_fp4(k: torch.Tensor, v: torch.Tensor, n_q_heads: int, page_size: int, head_dim: int) -> PagedLayer:
+    """View of one layer's 4-bit pages: k, v uint8 [n_pages][Hkv][fp4_page_bytes(page_size, head_dim)]."""
+    n, Hkv, size = k.shape
+    if v.shape != k.shape or size != fp4_page_bytes(page_size, head_dim):
+        raise LGError("paged_layer_fp4: needs k and v of one shape, %d bytes a page and head, got %s and %s" %
+                      (fp4_page_bytes(page_size, head_dim), tuple(k.shape), tuple(v.shape)))
+    dev = k.get_device()
+    if dev < 0:
+        raise LGError("paged_layer_fp4: needs device tensors")
+    l = PagedLayer(n, page_size, n_q_heads, Hkv, head_dim, LG_FP4, _need(k, torch.uint8, 1, dev, "k"),
+                   _need(v, torch.uint8, 1, dev, "v"))
+    l.tensors, l.device, l.torch_dtype = (k, v), dev, torch.uint8
+    return l
+
+
+def lg_rope_axes(sections: Sequence[int], order: int = LG_AXES_BLOCKS) -> torch.Tensor:
+    """The axis of each pair of a head, as an int32 tensor on the host."""
+    n = len(sections)
+    axis = torch.zeros(64, dtype=torch.int32)  # the most that the call writes
+    _check(_lib.lg_rope_axes(n, (ctypes.c_int32 * max(1, n))(*sections), order, axis.data_ptr()), "lg_rope_axes")
+    return axis[:sum(sections)].clone()
+
+
+def lg_rope_append_axes(layer: PagedLayer, m: PageMap, q, k, v, inv_freq, rot_dim: int, interleaved, scale: float, axis,
+                        coord, q_out, q_start, base, stream=None):
+    """axis, coord: int32 [rot_dim / 2] and [axes][total], or None both (positions of the map)."""
+    dev, D, i32 = m.device, layer.head_dim, torch.int32
+    stream = _on(dev, stream, layer)
+    x = q if q is not None else k
+    if x is None or (k is None) != (v is None) or (q is None) != (q_out is None):
+        raise LGError("lg_rope_append_axes: needs q with q_out, k with v, or all of them")
+    total, dt = x.shape[0], x.dtype
+    number = _number(dt, "lg_rope_append_axes")
+    qp = kp = vp = op = None
+    qs = ks = vs = 0
+    if q is not None:
+        qp, qs = _rows(q, layer.n_q_heads, D, dt, dev, "q")
+        op = _need(q_out, dt, total * layer.n_q_heads * D, dev, "q_out")
+    if k is not None:
+        if k.shape[0] != total or v.shape[0] != total:
+            raise LGError("lg_rope_append_axes: needs as many rows of k and v as of q")
+        kp, ks = _rows(k, layer.n_kv_heads, D, dt, dev, "k")
+        vp, vs = _rows(v, layer.n_kv_heads, D, dt, dev, "v")
+    fp = None if rot_dim == 0 else _need(inv_freq, torch.float32, rot_dim // 2, dev, "inv_freq")
+    ap = cp = None
+    n_axes = 0
+    if coord is not None or axis is not None:
+        if coord is None or axis is None or coord.dim() != 2 or coord.shape[1] < total:
+            raise LGError("lg_rope_append_axes: needs axis and coord [axes][rows], or neither")
+        n_axes = coord.shape[0]
+        ap, cp = _need(axis, i32, rot_dim // 2, dev, "axis"), _need(coord, i32, n_axes * total, dev, "coord")
+    _check(_lib.lg_rope_append_axes(ctypes.byref(layer), ctypes.byref(m), number, qp, qs, kp, ks, vp, vs, fp, rot_dim,
+                                    int(bool(interleaved)), scale, ap, cp, 0 if coord is None else coord.shape[1], n_axes, op,
+                                    _need(q_start, i32, m.batch + 1, dev, "q_start"),
+                                    _need(base, i32, m.batch, dev, "base"), total, stream),
+           "lg_rope_append_axes")
+
+
+def lg_page_unpack_fp4(layer: PagedLayer, m: PageMap, k_out, v_out, q_start, base, stream=None):
+    dev, i32 = m.device, torch.int32
+    stream = _on(dev, stream, layer)
+    x = k_out if k_out is not None else v_out
+    if x is None:
+        raise LGError("lg_page_unpack_fp4: needs k_out or v_out")
+    total, dt = x.shape[0], x.dtype
+    number, n = _number(dt, "lg_page_unpack_fp4"), total * layer.n_kv_heads * layer.head_dim
+    _check(_lib.lg_page_unpack_fp4(ctypes.byref(layer), ctypes.byref(m), number,
+                                   None if k_out is None else _need(k_out, dt, n, dev, "k_out"),
+                                   None if v_out is None else _need(v_out, dt, n, dev, "v_out"),
+                                   _need(q_start, i32, m.batch + 1, dev, "q_start"),
+                                   _need(base, i32, m.batch, dev, "base"), total, stream),
+           "lg_page_unpack_fp4")
+
+
+def lg_paged_attend_fp4_workspace(layer: PagedLayer, m: PageMap, dtype, total: int, max_chunk: int) -> int:
+    """dtype: torch.float32 or torch.bfloat16, of the queries."""
+    return int(_lib.lg_paged_attend_fp4_workspace(ctypes.byref(layer), ctypes.byref(m),
+                                                  _number(dtype, "lg_paged_attend_fp4_workspace"), total, max_chunk))
+
+
+def lg_paged_attend_fp4(layer: PagedLayer, m: PageMap, q, out, q_start, base, max_chunk: int, window: int, n_sink: int,
+                        suffix_w, lse, suffix_mass, conf, workspace, stream=None):
+    dev, B, dt, i32, f32 = m.device, m.batch, q.dtype, torch.int32, torch.float32
+    stream = _on(dev, stream, layer)
+    total, n = q.shape[0], q.shape[0] * layer.n_q_heads
+    ws, size = _bytes(workspace, dev, "workspace")
+    _check(_lib.lg_paged_attend_fp4(
+        ctypes.byref(layer), ctypes.byref(m), _number(dt, "lg_paged_attend_fp4"), _need(q, dt, n * layer.head_dim, dev, "q"),
+        _need(out, dt, n * layer.head_dim, dev, "out"), _need(q_start, i32, B + 1, dev, "q_start"),
+        _need(base, i32, B, dev, "base"), total, max_chunk, window, n_sink,
+        None if suffix_w is None else _need(suffix_w, i32, B, dev, "suffix_w"),
+        _need(lse, f32, n, dev, "lse"),
+        None if suffix_mass is None else _need(suffix_mass, f32, n, dev, "suffix_mass"),
+        None if conf is None else _need(conf, f32, B, dev, "conf"), ws, size, stream),
+        "lg_paged_attend_fp4")
 
 
 def params_from_dict(d) -> GuardParams:

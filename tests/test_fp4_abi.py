@@ -1,0 +1,238 @@
+"""The entry points of include/lg_fp4.h on the host: exported symbols, argument checks (nothing is enqueued, so these
+run without a GPU), workspace sizes, the axes of a head's pairs, and the model of 4-bit rows."""
+import ctypes
+import os
+import re
+import subprocess
+
+import numpy as np
+import pytest
+
+from oracle import fp4
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def _lg():
+    from paper_2604_10044_amd import lg
+    return lg
+
+
+def _map(lg, **kw):
+    return lg.PageMap(**dict(dict(batch=4, max_pages=8, n_pages=64, page_size=16, table=0x1000, pos=0x2000, len=0x3000, ref=0x4000), **kw))
+
+
+def _layer(lg, **kw):
+    return lg.PagedLayer(**dict(dict(n_pages=64, page_size=16, n_q_heads=8, n_kv_heads=2, head_dim=128, dtype=lg.LG_FP4,
+                                     k=0x10000, v=0x20000), **kw))
+
+
+def test_exports_every_declared_symbol():
+    lg = _lg()
+    src = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "lg_fp4.h")).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(lg_[a-z_0-9]+)\s*\(", src)))
+    assert len(names) == 5
+    out = subprocess.run(["nm", "-D", "--defined-only", lg.LIB_PATH], capture_output=True, text=True, check=True).stdout
+    exported = set(re.findall(r"\s[TW]\s+(lg_\w+)", out))
+    assert not [n for n in names if n not in exported]
+    assert all(hasattr(lg, n) and hasattr(lg._lib, n) for n in names)
+
+
+def test_header_compiles_as_c99(tmp_path):
+    src = tmp_path / "t.c"
+    src.write_text('#include "lg_fp4.h"\nint main(void) { lg_paged_layer l; l.dtype = LG_FP4; return l.dtype == LG_F32; }\n')
+    r = subprocess.run(["gcc", "-std=c99", "-Wall", "-Wextra", "-Werror", "-D__HIP_PLATFORM_AMD__", "-I",
+                        os.path.join(ROOT, "include"), "-I", "/opt/rocm/include", "-c", str(src), "-o", str(tmp_path / "t.o")],
+                       capture_output=True, text=True, timeout=120)
+    errors = [x for x in r.stderr.splitlines() if "lg_fp4.h" in x or "lg.h" in x]
+    assert not errors, errors
+
+
+BAD_MAPS = [(dict(table=None), 1), (dict(len=None), 1), (dict(ref=0x4004), 7), (dict(batch=0), 2), (dict(page_size=8), 3),
+            (dict(max_pages=1 << 27), 2)]
+BAD_LAYERS = [(dict(k=None), 1), (dict(v=0x20008), 7), (dict(n_pages=63), 2), (dict(page_size=32), 2), (dict(n_q_heads=7), 2),
+              (dict(n_q_heads=34), 3), (dict(head_dim=96), 3), (dict(dtype=2), 3), (dict(dtype=5), 3)]
+
+
+def _append(lg, l, m, dtype=None, **kw):
+    a = dict(q=0x10000, qs=1024, k=0x30000, ks=256, v=0x40000, vs=256, freq=0x100, rot=128, ilv=0, scale=1.0, axis=0x200, coord=0x300,
+             cs=5, axes=3, out=0x50000, q_start=0x10, base=0x20, total=5)
+    a.update(kw)
+    return lg._lib.lg_rope_append_axes(ctypes.byref(l), ctypes.byref(m), lg.LG_BF16 if dtype is None else dtype, a["q"], a["qs"], a["k"],
+                                       a["ks"], a["v"], a["vs"], a["freq"], a["rot"], a["ilv"], a["scale"], a["axis"], a["coord"],
+                                       a["cs"], a["axes"], a["out"], a["q_start"], a["base"], a["total"], None)
+
+
+def _unpack(lg, l, m, dtype=None, **kw):
+    a = dict(k=0x30000, v=0x40000, q_start=0x10, base=0x20, total=5)
+    a.update(kw)
+    return lg._lib.lg_page_unpack_fp4(ctypes.byref(l), ctypes.byref(m), lg.LG_BF16 if dtype is None else dtype, a["k"], a["v"],
+                                      a["q_start"], a["base"], a["total"], None)
+
+
+def _attend(lg, l, m, dtype=None, **kw):
+    a = dict(q=0x30000, out=0x40000, q_start=0x10, base=0x20, total=5, chunk=3, window=0, sink=0, w=0x30, lse=0x40, sm=0x50, conf=0x60,
+             ws=0x50000, size=1 << 34)
+    a.update(kw)
+    return lg._lib.lg_paged_attend_fp4(ctypes.byref(l), ctypes.byref(m), lg.LG_BF16 if dtype is None else dtype, a["q"], a["out"],
+                                       a["q_start"], a["base"], a["total"], a["chunk"], a["window"], a["sink"], a["w"], a["lse"],
+                                       a["sm"], a["conf"], a["ws"], a["size"], None)
+
+
+@pytest.mark.parametrize("call", [_append, _unpack, _attend])
+def test_maps_and_layers(call):
+    lg = _lg()
+    for kw, status in BAD_MAPS:
+        assert call(lg, _layer(lg), _map(lg, **kw)) == status, kw
+    for kw, status in BAD_LAYERS:
+        assert call(lg, _layer(lg, **kw), _map(lg)) == status, kw
+    n = 1 << 28
+    assert call(lg, _layer(lg, n_pages=n), _map(lg, n_pages=n)) == 2  # 2^32 slots
+    for dtype in (2, 3, lg.LG_FP4):
+        assert call(lg, _layer(lg), _map(lg), dtype=dtype) == 3
+    assert call(lg, _layer(lg), _map(lg), total=0) == 0
+    assert call(lg, _layer(lg), _map(lg), total=-1) == 2
+
+
+def test_append_arguments():
+    lg = _lg()
+    l, m = _layer(lg), _map(lg)
+    for kw in (dict(q_start=None), dict(base=None), dict(k=None), dict(v=None), dict(out=None), dict(q=None), dict(freq=None),
+               dict(axis=None), dict(coord=None), dict(q=None, out=None, k=None, v=None)):
+        assert _append(lg, l, m, **kw) == 1, kw
+    for kw in (dict(rot=-2), dict(rot=130), dict(rot=7), dict(axes=-1), dict(axes=9), dict(axes=0), dict(axes=0, axis=None),
+               dict(axes=0, coord=None), dict(out=0x10000, qs=1032)):
+        assert _append(lg, l, m, **kw) == 4, kw
+    for kw in (dict(qs=1023), dict(ks=255), dict(vs=255), dict(qs=(1 << 40) + 8), dict(cs=4), dict(cs=(1 << 40) + 1), dict(total=1 << 23, cs=1 << 23)):
+        assert _append(lg, l, m, **kw) == 2, kw
+    for kw in (dict(q=0x10008), dict(k=0x30008), dict(v=0x40004), dict(out=0x50008), dict(qs=1025), dict(ks=257), dict(vs=260)):
+        assert _append(lg, l, m, **kw) == 7, kw
+    # layers of other types take their own type alone
+    assert _append(lg, _layer(lg, dtype=lg.LG_BF16), m, dtype=lg.LG_F32) == 3
+    assert _append(lg, _layer(lg, dtype=lg.LG_F32), m, dtype=lg.LG_BF16) == 3
+    assert _append(lg, _layer(lg, dtype=lg.LG_BF16), m, total=0) == 0
+
+
+def test_unpack_arguments():
+    lg = _lg()
+    l, m = _layer(lg), _map(lg)
+    for kw in (dict(k=None, v=None), dict(q_start=None), dict(base=None)):
+        assert _unpack(lg, l, m, **kw) == 1, kw
+    assert _unpack(lg, l, m, k=0x30000, v=0x30000) == 4
+    assert _unpack(lg, l, m, total=1 << 23) == 2
+    for kw in (dict(k=0x30008), dict(v=0x40002)):
+        assert _unpack(lg, l, m, **kw) == 7, kw
+    for t in (lg.LG_F32, lg.LG_BF16):
+        assert _unpack(lg, _layer(lg, dtype=t), m) == 3
+
+
+def test_attend_arguments():
+    lg = _lg()
+    l, m = _layer(lg), _map(lg)
+    for kw in (dict(q=None), dict(out=None), dict(q_start=None), dict(base=None), dict(lse=None), dict(w=None), dict(w=None, sm=None),
+               dict(w=None, conf=None), dict(ws=None)):
+        assert _attend(lg, l, m, **kw) == 1, kw
+    for kw in (dict(window=-1), dict(sink=-1), dict(out=0x30000)):
+        assert _attend(lg, l, m, **kw) == 4, kw
+    for kw in (dict(q=0x30008), dict(out=0x40008), dict(ws=0x50008)):
+        assert _attend(lg, l, m, **kw) == 7, kw
+    for kw in (dict(chunk=-1), dict(total=1 << 28)):
+        assert _attend(lg, l, m, **kw) == 2, kw
+    for t in (lg.LG_F32, lg.LG_BF16):
+        assert _attend(lg, _layer(lg, dtype=t), m) == 3
+
+
+def test_other_calls_on_4_bit_layers():
+    """The calls of lg_paged.h that rotate and attend refuse 4-bit layers; lg.h has none."""
+    lg = _lg()
+    l, m = _layer(lg), _map(lg)
+    f = lg._lib.lg_rope_append
+    assert f(ctypes.byref(l), ctypes.byref(m), 0x10000, 1024, 0x30000, 256, 0x40000, 256, 0x100, 128, 0, 1.0, 0x50000, 0x10, 0x20, 5,
+             None) == 3
+    assert lg._lib.lg_paged_attend(ctypes.byref(l), ctypes.byref(m), 0x30000, 0x40000, 0x10, 0x20, 5, 3, 0, 0, 0x30, 0x40, 0x50, 0x60,
+                                   0x50000, 1 << 34, None) == 3
+    assert lg.lg_paged_attend_workspace(l, m, 5, 3) == 0
+    c = lg.LayerCache(2, 8, 2, 128, 64, lg.LG_FP4, 0x10000, 0x20000, 0x30000)
+    assert lg.lg_decode_attend_workspace(c) == 0
+    # one type a call
+    arr = (lg.PagedLayer * 2)(l, _layer(lg, dtype=lg.LG_BF16))
+    assert lg._lib.lg_page_reserve(ctypes.byref(m), 2, arr, 0x10, 0x20, 0x30, 0x50000, 1 << 30, None) == 2
+
+
+def test_workspace_covers_smaller_steps():
+    """The size for the largest step serves every smaller one, and too little is refused."""
+    import torch
+    lg = _lg()
+    bf, f32 = torch.bfloat16, torch.float32
+    for hq, hkv, D in ((8, 2, 128), (28, 4, 128), (4, 4, 64), (15, 3, 64), (16, 1, 128)):
+        for B, P in ((1, 4096), (3, 700), (32, 128), (200, 8)):
+            m = _map(lg, batch=B, max_pages=P)
+            l = _layer(lg, n_q_heads=hq, n_kv_heads=hkv, head_dim=D)
+            for dt, number in ((bf, lg.LG_BF16), (f32, lg.LG_F32)):
+                most = lg.lg_paged_attend_fp4_workspace(l, m, dt, 4 * B + 600, 600)
+                assert most >= 16 and most % 16 == 0
+                for total, chunk in ((1, 1), (B, 1), (B, 4), (4 * B, 4), (B + 50, 51), (600, 600), (4 * B + 600, 600)):
+                    size = lg.lg_paged_attend_fp4_workspace(l, m, dt, total, chunk)
+                    assert 16 <= size <= most, (hq, hkv, D, B, P, total, chunk)
+    assert lg.lg_paged_attend_fp4_workspace(_layer(lg, dtype=lg.LG_BF16), m, bf, 5, 3) == 0
+    with pytest.raises(lg.LGError):
+        lg.lg_paged_attend_fp4_workspace(_layer(lg), m, torch.float16, 5, 3)
+
+
+def test_axes():
+    lg = _lg()
+    f = lg.lg_rope_axes
+    assert f([2, 3, 1]).tolist() == [0, 0, 1, 1, 1, 2]
+    assert f([2, 3, 1], lg.LG_AXES_TURNS).tolist() == [0, 1, 2, 0, 1, 1]
+    assert f([0, 2], lg.LG_AXES_TURNS).tolist() == [1, 1]
+    assert f([0, 0, 4, 0]).tolist() == [2] * 4
+    assert f([64]).tolist() == [0] * 64
+    t = f([16, 24, 24], lg.LG_AXES_TURNS).tolist()
+    assert t[:48] == [0, 1, 2] * 16 and t[48:] == [1, 2] * 8
+    for bad in ([], [0], [0, 0], [65], [32, 33], [-1, 5], [1] * 9):
+        with pytest.raises(lg.LGError):
+            f(bad)
+    with pytest.raises(lg.LGError):
+        f([4, 4], 2)
+    assert lg._lib.lg_rope_axes(2, None, 0, 0x10) == 1
+
+
+def test_binding_refuses_host_tensors():
+    import torch
+    lg = _lg()
+    k = torch.zeros(4, 2, lg.fp4_page_bytes(16, 64), dtype=torch.uint8)
+    with pytest.raises(lg.LGError):
+        lg.paged_layer_fp4(k, k, 4, 16, 64)
+    with pytest.raises(lg.LGError):
+        lg.paged_layer_fp4(k, k, 4, 16, 128)
+    with pytest.raises(lg.LGError):
+        lg.paged_layer_fp4(k, k[:3], 4, 16, 64)
+
+
+def test_the_model_of_rows():
+    """The oracle against the definition's own examples: units, ties, saturation, what is not finite."""
+    x = np.zeros((8, 32))
+    x[0, :9] = [6, 5, 2.5, 3.5, 0.25, 0.75, -1.25, -1.75, 0.2500001]
+    x[1, :3] = [6.0000001, 1, -0.5]
+    x[2, 0] = 3.0
+    x[3, 0] = 1e-45
+    x[4, :2] = [3.3e38, -1e38]
+    x[5, 3] = np.inf
+    x[6, 31] = np.nan
+    codes, exps = fp4.encode(x)
+    assert exps[:, 0].tolist() == [127, 128, 126, 2, 252, 255, 255, 2]
+    v = fp4.values(codes, exps)
+    assert v[0, :9].tolist() == [6, 4, 2, 4, 0, 1, -1, -2, 0.5]
+    assert v[1, :3].tolist() == [6, 1, -0.0] and v[2, 0] == 3 and v[3, 0] == 0
+    assert v[4, 0] == 6 * 2.0 ** 125 and v[4, 1] == -2 * 2.0 ** 125
+    assert np.isnan(v[5:7]).all() and (v[7] == 0).all()
+    r = np.random.RandomState(0).randn(50, 2, 16, 128) * 10.0 ** np.random.RandomState(1).randint(-20, 20, (50, 2, 16, 1))
+    codes, exps = fp4.encode(r)
+    unit = np.repeat(2.0 ** (exps - 127.0), 32, -1)
+    y = fp4.values(codes, exps)
+    assert (np.abs(y - r) <= unit).all() and (np.abs(y - r)[np.abs(r) <= 2 * unit] <= (unit / 4)[np.abs(r) <= 2 * unit]).all()
+    assert (np.abs(r).reshape(50, 2, 16, 4, 32).max(-1) > 3 * 2.0 ** (exps - 127.0)).all()
+    b = fp4.pack(codes, exps)
+    assert b.shape == (50, 2, 16 * 68)
+    for p, q in zip(fp4.unpack(b, 16, 128), (codes, exps)):
+        np.testing.assert_array_equal(p, q)
