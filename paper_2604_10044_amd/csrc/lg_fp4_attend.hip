@@ -1,129 +1,929 @@
 // lg_fp4_attend.hip -- attention of a step's new tokens over 4-bit pages (lg_paged_attend_fp4).
 //
-// A wave a query row (a token's query head): 64 slots at a time, a lane forms the score of one, then the lanes hold
-// D / 64 values of the output each and add up the 64 weighted values, with the running maximum and sum of a softmax.
+// The mathematics, the workgroups' rows and slots and the running maximum are those of lg_paged_attend.hip: a wave takes
+// query rows of one KV head of one sequence and walks tiles of slots with
+//   S^T = K Q^T,  m' = max(m, max S),  P = 2^(S - m'),  l = l 2^(m - m') + sum P,  O^T = O^T 2^(m - m') + V^T P^T.
+// A 4-bit number times its power of two is a bfloat16 number exactly, and one instruction makes two of them. So K
+// and V become bfloat16 in registers, and both products are bfloat16 matrix instructions whose products are exact. float32
+// queries and weights enter as three bfloat16 terms each (8 + 8 + 8 bits, exact), three times the instructions, still
+// a fifth of what float32 ones would take.
 #include "lg_fp4.h"
-#include "lg_paged_internal.h"
+#include "lg_paged_attend.h"
 
 namespace lg {
 
-struct Fp4AttendArgs {
-  const void* q;
-  const char *k, *v;
-  void* out;
-  const int32_t *q_start, *base, *suffix_w;
-  float *lse, *suffix, *conf;
-  MapArgs map;
-  int32_t Hq, Hkv, G, D, total, max_chunk, window, n_sink;
-  float scale_log2;
-};
-
-constexpr int kRowThreads = 64;
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-__device__ __forceinline__ float wave_max(float x) {
-  for (int o = 1; o < 64; o <<= 1) x = fmaxf(x, __shfl_xor(x, o, 64));
-  return x;
+// ------------------------------------------------------------------------------------------
+// Terms
+// ------------------------------------------------------------------------------------------
+// Terms of a query, and of a weight in steps of few rows and in chunks (see lg_paged_attend.hip for bfloat16 calls' one
+// and two).
+template <typename T> constexpr int q_terms() { return sizeof(T) == 4 ? 3 : 1; }
+template <typename T, bool FEW> constexpr int p_terms() { return sizeof(T) == 4 ? 3 : FEW ? 2 : 1; }
+
+// Two weights as N bfloat16 terms, each what the ones before leave, to nearest: with two within 2^-17, with three exact.
+template <int N>
+__device__ __forceinline__ void weight_terms(float x, float y, uint32_t (&t)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    t[i] = pack_bf16(x, y);
+    if (i + 1 < N) {
+      x -= __uint_as_float(t[i] << 16);
+      y -= __uint_as_float(t[i] & 0xffff0000u);
+    }
+  }
 }
-__device__ __forceinline__ float wave_sum(float x) {
-  for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o, 64);
-  return x;
+
+// 8 values of a query as N terms. float32: cut off after 8 and 16 bits, so that no term is larger than the value; one that
+// is not finite is its first term alone.
+template <typename T, int N>
+__device__ __forceinline__ void load_query(const T* src, u32x4_t (&t)[N]) {
+  if constexpr (N == 1) {
+    t[0] = *(const u32x4_t*)src;
+  } else {
+    const f32x4 a = *(const f32x4*)src, b = *(const f32x4*)(src + 4);
+    const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t w[N] = {};
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float y = x[2 * i + e];
+        const bool finite = (__float_as_uint(y) & 0x7f800000u) != 0x7f800000u;
+        if (!finite) {
+          w[0] |= (pack_bf16(y, y) & 0xffffu) << (16 * e);
+        } else {
+#pragma unroll
+          for (int n = 0; n < N; ++n) {
+            const uint32_t top = __float_as_uint(y) & 0xffff0000u;
+            w[n] |= e == 0 ? top >> 16 : top;
+            y -= __uint_as_float(top);
+          }
+        }
+      }
+#pragma unroll
+      for (int n = 0; n < N; ++n) t[n][i] = w[n];
+    }
+  }
+}
+
+// 8 values of a word of codes as bfloat16.
+__device__ __forceinline__ u32x4_t decode(uint32_t codes, float unit) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 1);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, unit, 3);
+  return u32x4_t{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b), __builtin_bit_cast(uint32_t, c),
+                 __builtin_bit_cast(uint32_t, d)};
+}
+
+__device__ __forceinline__ f32x4 mfma16(u32x4_t a, u32x4_t b, f32x4 c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 mfma32(u32x4_t a, u32x4_t b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// 4 keys x 16 values of bfloat16 in LDS, a lane 4 values of a key; each lane gets one value of 4 keys.
+__device__ __forceinline__ u32x2_t read_turned(const char* at) {
+  return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
+}
+
+// ------------------------------------------------------------------------------------------
+// Tiles
+// ------------------------------------------------------------------------------------------
+struct Look {
+  int page, pos;  // of the lane's slot
+};
+
+// The rows of a tile that a workgroup or wave works on, as slots.
+template <int NK>
+struct Walk {
+  const PagedAttendArgs& a;
+  const Job& job;
+  const int32_t *table, *pos;
+  int last_slot;  // the last one that any of the rows sees
+
+  __device__ __forceinline__ int slot_of(int t) const { return (t < job.sink_tiles ? t : t - job.sink_tiles + job.tile0) * NK; }
+  // Columns and positions of a tile, a lane a slot; slots behind last_slot read as last_slot: no row sees them.
+  __device__ __forceinline__ Look look(int t) const {
+    const int s = min(slot_of(min(t, job.t_end - 1)) + ((int)threadIdx.x & (NK - 1)), last_slot);
+    return {table[s >> a.map.shift], pos[s]};
+  }
+};
+
+// 16 rows of one page: where their block begins, the first row in it, and the rows that there are behind that.
+struct Rows16 {
+  size_t block;
+  int row, most;
+};
+__device__ __forceinline__ Rows16 rows16(const PagedAttendArgs& a, const Job& job, int page, int slot, int last_slot, size_t block) {
+  Rows16 r;
+  page = is_page(a.map, page) ? page : 0;
+  slot = min(slot, last_slot & ~15);
+  r.block = ((size_t)page * a.Hkv + job.h) * block;
+  r.row = slot & ((1 << a.map.shift) - 1);
+  r.most = last_slot - slot;
+  return r;
+}
+
+// What a row of the wave sees: slots up to its own, at positions above win or below n_sink; it counts those above
+// suf as its suffix.
+struct Sight {
+  int slot, win, suf;
+};
+__device__ __forceinline__ Sight sight_of(const PagedAttendArgs& a, const Job& job, const int32_t* pos, int tok) {
+  Sight s;
+  s.slot = job.base + tok;
+  const int p = pos[s.slot], sw = a.suffix_w != nullptr ? a.suffix_w[job.b] : 0;
+  s.win = a.window > 0 ? (int)max((long long)p - a.window, (long long)INT32_MIN) : INT32_MIN;
+  s.suf = (int)max((long long)p - max(sw, 0), (long long)INT32_MIN);
+  return s;
+}
+
+__device__ __forceinline__ bool sees(const PagedAttendArgs& a, const Sight& s, int slot, int p) {
+  return slot <= s.slot && p != kHidden && (a.window == 0 || p > s.win || p < a.n_sink);
+}
+
+// How a tile of NK slots from s0 on, with the lane's slot at position tp, is to be compared: whether some row may not
+// see a slot (lo: the first row's own slot, win_hi: the last row's window), and what it has of the suffix.
+enum { kNone, kAll, kSome };
+template <int NK>
+__device__ __forceinline__ bool is_masked(const PagedAttendArgs& a, int tp, int s0, int lo, int win_hi) {
+  const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
+  return __ballot(tp == kHidden) != 0 || s0 + NK - 1 > lo || (a.window > 0 && p_first <= win_hi && p_last >= a.n_sink);
+}
+template <int NK>
+__device__ __forceinline__ int suffix_of(const PagedAttendArgs& a, int tp, int suf_lo, int suf_hi) {
+  if (a.suffix == nullptr && a.conf == nullptr) return kNone;
+  const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
+  // kHidden in front says nothing about the slots behind it
+  return p_last <= suf_lo ? kNone : p_first > suf_hi && p_first != kHidden ? kAll : kSome;
+}
+
+// LDS of a wave beside its tiles: 64 bounds (a row sees slot j if bound_j > win and the slot is none behind its own), 64
+// positions.
+constexpr int kNotes = 512;
+__device__ __forceinline__ void note(const PagedAttendArgs& a, int32_t* notes, int tp) {
+  const int lane = threadIdx.x & 63;
+  notes[lane] = tp == kHidden ? INT32_MIN : a.window == 0 || tp < a.n_sink ? INT32_MAX : tp;
+  notes[64 + lane] = tp;
+}
+
+// ------------------------------------------------------------------------------------------
+// Few rows
+// ------------------------------------------------------------------------------------------
+// At most 16 NR query rows of a sequence (a decode step: G rows), KW waves that take every KW-th tile of 32 slots each,
+// with no barrier until their (m, l, O) are joined. Matrix instructions of 16 rows: a lane holds 4 of every 16 keys of ONE
+// row, the four lanes of a row are 16 apart. K comes from memory as the first product's operand: the order of the
+// dimensions in a product is free, so a lane takes a quarter of its key's row as it lies (with 128 dimensions, one
+// group). V passes through LDS as bfloat16 and is read transposed.
+constexpr int kFewKeys = 32;
+
+template <int DV, int NR>
+struct Few {
+  static constexpr int kTile = kFewKeys * DV * 2;
+  static constexpr int kStat = 16 * NR * (DV + 4);  // floats of a wave's O, [row][DV + 4], before its m, l, suffix sums
+  static constexpr int kJoin = (kStat + 3 * 16 * NR) * 4;
+  static constexpr int kLds = ((kTile + kNotes > kJoin ? kTile + kNotes : kJoin) + 255) & ~255;
+  // 16-byte pieces of a row of V lie in the order piece ^ turn(row): the 4 rows that 16 lanes write and the 8 rows of 32
+  // bytes that 32 lanes read then lie in different banks.
+  static __device__ __forceinline__ int turn(int row) {
+    return DV == 128 ? 2 * (row & 7) | ((row >> 1) & 1) : 2 * ((row >> 1) & 3) | ((row >> 2) & 1);
+  }
+};
+
+template <typename T, int D, int KW, int DV, int NR>
+__device__ __forceinline__ void few_body(const PagedAttendArgs& a, Job job, char* lds) {
+  using C = Few<DV, NR>;
+  constexpr int QT = q_terms<T>(), PT = p_terms<T, true>();
+  constexpr int NK = kFewKeys, NJ = NK / 16, NKK = D / 32, ND = DV / 16;
+  constexpr int RB = D / 2, EB = D / 32;    // bytes of a row and of its exponents
+  constexpr int VP = DV / 32, VU = NK * VP / 64;  // groups of a row of V, and of them a lane's
+  constexpr int RBV = 2 * DV;
+  using KRow = std::conditional_t<D == 128, u32x4_t, u32x2_t>;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int part = lane >> 4, col = lane & 15;
+  char* const my = lds + wave * C::kLds;
+  int32_t* const notes = (int32_t*)(my + C::kTile);
+  const size_t block = fp4_block(D, a.map.shift);
+  const int ps = 1 << a.map.shift;
+  Walk<NK> walk = {a, job, a.map.table + (size_t)job.b * a.map.P, a.map.pos + (size_t)job.b * a.map.cap,
+                   job.base + (job.rows - 1) / a.G};
+  const int32_t* const pos = walk.pos;
+  const int last_slot = walk.last_slot;
+
+  int t_first = job.t_begin + wave;
+  Look l0 = {}, l1 = {};
+  if (t_first < job.t_end) l0 = walk.look(t_first);
+  u32x4_t qf[NR][NKK][QT];
+  Sight sight[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const int R = min(16 * n + col, job.rows - 1), tok = R / a.G;  // rows behind the last repeat it; they are not written
+    const T* src = (const T*)a.q + ((size_t)(job.first + tok) * a.Hq + job.h * a.G + R - tok * a.G) * D + part * (D / 4);
+#pragma unroll
+    for (int k = 0; k < NKK; ++k) load_query<T, QT>(src + 8 * k, qf[n][k]);
+    sight[n] = sight_of(a, job, pos, tok);
+  }
+  if (skip_hidden<NK>(a, job, pos)) {
+    t_first = job.t_begin + wave;
+    if (t_first < job.t_end) l0 = walk.look(t_first);
+  }
+  // the first and the last row's
+  const Sight lo = sight_of(a, job, pos, 0), hi = sight_of(a, job, pos, (job.rows - 1) / a.G);
+
+  f32x4 O[NR][ND];
+  float mx[NR], l[NR], sfx[NR];  // l and sfx: the lane's share of the keys
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+#pragma unroll
+    for (int d = 0; d < ND; ++d) O[n][d] = f32x4{0.f, 0.f, 0.f, 0.f};
+    mx[n] = -INFINITY;
+    l[n] = sfx[n] = 0.f;
+  }
+
+  struct Raw {
+    KRow k[NJ];
+    u32x4_t v[VU];
+    uint32_t ke[NJ], ve[VU];
+  };
+  auto load = [&](int t, const Look& lk) __attribute__((always_inline)) {
+    Raw raw;
+    Rows16 r[NJ];
+    const int s0 = walk.slot_of(t);
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      r[j] = rows16(a, job, __builtin_amdgcn_readlane(lk.page, 16 * j), s0 + 16 * j, last_slot, block);
+      const int row = r[j].row + min(col, r[j].most);
+      const char* at = (const char*)a.k + r[j].block;
+      raw.k[j] = *(const KRow*)(at + row * RB + part * (RB / 4));
+      raw.ke[j] = *(const uint8_t*)(at + ps * RB + row * EB + (D == 128 ? part : part >> 1));
+    }
+#pragma unroll
+    for (int u = 0; u < VU; ++u) {
+      const int in = lane / VP + u * (64 / VP);  // row of the tile
+      const bool second = VP == 4 ? u & 1 : in >= 16;
+      const size_t first = second ? r[1].block : r[0].block;
+      const int row = (second ? r[1].row : r[0].row) + min(in & 15, second ? r[1].most : r[0].most);
+      const char* at = (const char*)a.v + first;
+      raw.v[u] = *(const u32x4_t*)(at + row * RB + job.d0 / 2 + lane % VP * 16);
+      raw.ve[u] = *(const uint8_t*)(at + ps * RB + row * EB + job.d0 / 32 + lane % VP);
+    }
+    return raw;
+  };
+
+  const int v_row = lane / VP, v_write = v_row * RBV, v_turn = C::turn(v_row);
+  const int k_row = 4 * part + (col >> 2);
+  const char* const v_read = my + k_row * RBV + 16 * (((col & 3) >> 1) ^ C::turn(k_row)) + 8 * (col & 1);
+
+  auto tile = [&](int t, const Look& lk, const Raw& raw) __attribute__((always_inline)) {
+    const int s0 = walk.slot_of(t);
+    const int tp = is_page(a.map, lk.page) ? lk.pos : kHidden;
+    // V as bfloat16
+#pragma unroll
+    for (int u = 0; u < VU; ++u) {
+      u32x4_t codes = raw.v[u];
+      const unsigned long long odd = __ballot(raw.ve[u] > 252);
+      if (odd != 0) {
+        // Groups that stand for NaN: 0 in the product, and NaN in their 32 values of the rows that see the slot.
+        if (raw.ve[u] > 252) codes = u32x4_t{0, 0, 0, 0};
+        for (unsigned long long left = odd; left != 0; left &= left - 1) {
+          const int bit = __builtin_ctzll(left), key = bit / VP + u * (64 / VP), g = bit % VP;
+          const int p = __builtin_amdgcn_readlane(tp, key);
+#pragma unroll
+          for (int n = 0; n < NR; ++n) {
+            const bool see = sees(a, sight[n], s0 + key, p);
+#pragma unroll
+            for (int d = 0; d < ND; ++d)
+              if (d / 2 == g && see) O[n][d] = f32x4{NAN, NAN, NAN, NAN};
+          }
+        }
+      }
+      const float unit = fp4_unit(raw.ve[u] > 252 ? 127 : raw.ve[u]);
+#pragma unroll
+      for (int w = 0; w < 4; ++w)
+        *(u32x4_t*)(my + u * (64 / VP) * RBV + v_write + 16 * ((4 * (lane % VP) + w) ^ v_turn)) = decode(codes[w], unit);
+    }
+    f32x4 S[NR][NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) {
+      const float unit = fp4_unit(raw.ke[j]);
+#pragma unroll
+      for (int n = 0; n < NR; ++n) S[n][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int k = 0; k < NKK; ++k) {
+        const u32x4_t x = decode(raw.k[j][k], unit);
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int i = 0; i < QT; ++i) S[n][j] = mfma16(x, qf[n][k][i], S[n][j]);
+      }
+    }
+    const bool masked = is_masked<NK>(a, tp, s0, lo.slot, hi.win);
+    const int how = suffix_of<NK>(a, tp, lo.suf, hi.suf);
+    if (masked || how == kSome) note(a, notes, tp);
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const i32x4 bound = *(const i32x4*)(notes + 16 * j + 4 * part);
+#pragma unroll
+        for (int n = 0; n < NR; ++n) {
+          const int last = sight[n].slot - s0 - 16 * j - 4 * part;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) S[n][j][i] = bound[i] > sight[n].win && i <= last ? S[n][j][i] : -INFINITY;
+        }
+      }
+    }
+    uint32_t P[NR][NK / 32][4][PT];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+      float top = fmaxf(fmaxf(S[n][0][0], S[n][0][1]), fmaxf(S[n][0][2], S[n][0][3]));
+#pragma unroll
+      for (int j = 1; j < NJ; ++j) top = fmaxf(top, fmaxf(fmaxf(S[n][j][0], S[n][j][1]), fmaxf(S[n][j][2], S[n][j][3])));
+      top = fmaxf(top, other_row(top));
+      top = fmaxf(top, other_half(top)) * a.scale_log2;
+      // The running maximum follows only when a score passes it by kSlack (weights are then at most 2^kSlack).
+      const bool raise = top > mx[n] + kSlack;
+      if (__any(raise)) {
+        const float f = raise ? __builtin_amdgcn_exp2f(mx[n] - top) : 1.f;  // 0 where nothing was seen before
+        mx[n] = raise ? top : mx[n];
+        l[n] *= f;
+        sfx[n] *= f;
+#pragma unroll
+        for (int d = 0; d < ND; ++d) O[n][d] *= f;
+      }
+      const float off = mx[n] == -INFINITY ? 0.f : -mx[n];
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[n][j][i] = __builtin_amdgcn_exp2f(fmaf(S[n][j][i], a.scale_log2, off));
+        sum += (S[n][j][0] + S[n][j][1]) + (S[n][j][2] + S[n][j][3]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) weight_terms<PT>(S[n][j][2 * i], S[n][j][2 * i + 1], P[n][j / 2][2 * (j & 1) + i]);
+      }
+      l[n] += sum;
+      sfx[n] += how == kAll ? sum : 0.f;
+      if (how == kSome) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const i32x4 p = *(const i32x4*)(notes + 64 + 16 * j + 4 * part);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sfx[n] += p[i] > sight[n].suf ? S[n][j][i] : 0.f;
+        }
+      }
+    }
+    // O^T += V^T P^T: the lane's keys of a product are 4 part .. and 16 + 4 part ..
+#pragma unroll
+    for (int s = 0; s < NK / 32; ++s)
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const char* at = my + (((int)(v_read - my) + 32 * s * RBV) ^ (32 * d));
+        const u32x2_t x = read_turned(at), y = read_turned(at + 16 * RBV);
+        const u32x4_t z = {x[0], x[1], y[0], y[1]};
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+          for (int i = 0; i < PT; ++i)
+            O[n][d] = mfma16(z, u32x4_t{P[n][s][0][i], P[n][s][1][i], P[n][s][2][i], P[n][s][3][i]}, O[n][d]);
+      }
+  };
+
+  if (t_first < job.t_end) {
+    l1 = walk.look(t_first + KW);
+    Raw raw = load(t_first, l0);
+    for (int t = t_first; t < job.t_end; t += KW) {
+      Raw next = raw;
+      if (t + KW < job.t_end) next = load(t + KW, l1);
+      const Look l2 = walk.look(t + 2 * KW);
+      tile(t, l0, raw);
+      raw = next;
+      l0 = l1;
+      l1 = l2;
+    }
+  }
+
+  // Join the waves: their numerators and statistics through LDS.
+  constexpr int kRows = 16 * NR, kParts = 64 * KW / kRows, kPairs = DV / (2 * kParts);
+  float* const num = (float*)my;
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    l[n] += other_row(l[n]);
+    l[n] += other_half(l[n]);
+    sfx[n] += other_row(sfx[n]);
+    sfx[n] += other_half(sfx[n]);
+#pragma unroll
+    for (int d = 0; d < ND; ++d) *(f32x4*)(num + (16 * n + col) * (DV + 4) + 16 * d + 4 * part) = O[n][d];
+    if (part == 0) {
+      num[C::kStat + 16 * n + col] = mx[n];
+      num[C::kStat + kRows + 16 * n + col] = l[n];
+      num[C::kStat + 2 * kRows + 16 * n + col] = sfx[n];
+    }
+  }
+  __syncthreads();
+  auto row_of = [&](int r) __attribute__((always_inline)) {
+    const int tk = r / a.G;
+    return (size_t)(job.first + tk) * a.Hq + job.h * a.G + (r - tk * a.G);
+  };
+  const size_t split0 = (size_t)job.split * a.total * a.Hq;
+  if (wave == KW - 1 && job.d0 == 0) {  // the statistics, a lane a row
+    const int r = min(lane, job.rows - 1);
+    float M = -INFINITY, L = 0.f, SF = 0.f;
+#pragma unroll
+    for (int w = 0; w < KW; ++w) M = fmaxf(M, ((const float*)(lds + w * C::kLds))[C::kStat + r]);
+    const float Ms = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int w = 0; w < KW; ++w) {
+      const float* src = (const float*)(lds + w * C::kLds) + C::kStat + r;
+      const float f = __builtin_amdgcn_exp2f(src[0] - Ms);
+      L += f * src[kRows];
+      SF += f * src[2 * kRows];
+    }
+    const bool own = lane < job.rows;
+    const size_t row = row_of(r);
+    if (a.ns > 1) {
+      if (own) *(f32x4*)(a.pml + (split0 + row) * 4) = f32x4{M, L, SF, 0.f};
+    } else {
+      const float mass = L == 0.f ? 0.f : SF * (1.f / L);
+      if (own) {
+        a.lse[row] = L == 0.f ? -INFINITY : kLn2 * (M + __builtin_amdgcn_logf(L));
+        if (a.suffix != nullptr) a.suffix[row] = mass;
+      }
+      if (a.conf != nullptr) raise_conf(a.conf + job.b, mass, r / a.G == job.rows / a.G - 1);
+    }
+  }
+  const int r = tid / kParts, share = tid % kParts;
+  if (r >= job.rows) return;
+  float wm[KW], M = -INFINITY;
+#pragma unroll
+  for (int w = 0; w < KW; ++w) {
+    wm[w] = ((const float*)(lds + w * C::kLds))[C::kStat + r];
+    M = fmaxf(M, wm[w]);
+  }
+  const float Ms = M == -INFINITY ? 0.f : M;
+  float L = 0.f;
+  f32x2 x[kPairs] = {};
+#pragma unroll
+  for (int w = 0; w < KW; ++w) {
+    const float* src = (const float*)(lds + w * C::kLds);
+    const float f = __builtin_amdgcn_exp2f(wm[w] - Ms);
+    L += f * src[C::kStat + kRows + r];
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) x[i] += f * *(const f32x2*)(src + r * (DV + 4) + 2 * (kParts * i + share));
+  }
+  const size_t row = row_of(r);
+  if (a.ns > 1) {
+#pragma unroll
+    for (int i = 0; i < kPairs; ++i) *(f32x2*)(a.po + (split0 + row) * D + job.d0 + 2 * (kParts * i + share)) = x[i];
+    return;
+  }
+  const float inv = 1.f / L;
+  T* dst = (T*)a.out + row * D + job.d0;
+#pragma unroll
+  for (int i = 0; i < kPairs; ++i) {
+    const float y0 = L == 0.f ? 0.f : x[i][0] * inv, y1 = L == 0.f ? 0.f : x[i][1] * inv;
+    if constexpr (sizeof(T) == 4)
+      *(f32x2*)(dst + 2 * (kParts * i + share)) = f32x2{y0, y1};
+    else
+      *(uint32_t*)(dst + 2 * (kParts * i + share)) = pack_bf16(y0, y1);
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// Many rows
+// ------------------------------------------------------------------------------------------
+// 128 query rows of a sequence, four waves of 32, which share every tile of 64 slots: a thread brings a quarter of a row of
+// K and of V as bfloat16 to LDS, while the tile before is multiplied (two buffers, one barrier a tile). From there on it is
+// the bfloat16 kernel's walk, in its layout but for V's turn.
+constexpr int kManyKeys = 64;
+
+template <int D>
+struct Many {
+  static constexpr int kRow = 2 * D, kTile = kManyKeys * kRow, kBuffer = 2 * kTile;
+  static constexpr int kFlags = 2 * kBuffer;  // a byte a quarter of a row of V, two buffers: it stands for NaN
+  static constexpr int kOwnNotes = kFlags + 2 * 256;
+  static constexpr int kLds = kOwnNotes + 4 * kNotes;
+  // 16-byte pieces of a row lie in the order piece ^ turn(row): K for the 16 rows of a read, V for the 4 rows (of 64 bytes)
+  // of a transposed one, both also for the 4 rows that 16 lanes write.
+  static __device__ __forceinline__ int turn_k(int row) { return D == 128 ? row & 15 : (row >> 1) & 7; }
+  static __device__ __forceinline__ int turn_v(int row) { return 5 * (D == 128 ? row & 3 : (row >> 1) & 1); }
+};
+
+template <typename T, int D>
+__device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, char* lds) {
+  using C = Many<D>;
+  constexpr int QT = q_terms<T>(), PT = p_terms<T, false>();
+  constexpr int NK = kManyKeys, ND = D / 32, RB = D / 2, EB = D / 32, RBV = C::kRow;
+  using Quarter = std::conditional_t<D == 128, u32x4_t, u32x2_t>;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int part = lane >> 5, col = lane & 31;
+  int32_t* const notes = (int32_t*)(lds + C::kOwnNotes + wave * kNotes);
+  const size_t block = fp4_block(D, a.map.shift);
+  const int ps = 1 << a.map.shift;
+  Walk<NK> walk = {a, job, a.map.table + (size_t)job.b * a.map.P, a.map.pos + (size_t)job.b * a.map.cap,
+                   job.base + (min(job.row0 + kManyRows, job.rows) - 1) / a.G};
+  const int32_t* const pos = walk.pos;
+  const int last_slot = walk.last_slot;
+
+  const int wrow0 = job.row0 + wave * kWaveRows;
+  const int R = wrow0 + col;
+  const bool live = R < job.rows, idle = wrow0 >= job.rows;  // a wave without rows only loads
+  const int Rc = live ? R : job.rows - 1, tok = Rc / a.G;    // rows behind the last repeat it; they are not written
+  const size_t qrow = (size_t)(job.first + tok) * a.Hq + job.h * a.G + Rc - tok * a.G;
+  Look l0 = {}, l1 = {}, l2 = {};
+  if (job.t_begin < job.t_end) l0 = walk.look(job.t_begin);
+  u32x4_t qf[D / 16][QT];
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) load_query<T, QT>((const T*)a.q + qrow * D + 16 * k + 8 * part, qf[k]);
+  const Sight sight = sight_of(a, job, pos, tok);
+  if (skip_hidden<NK>(a, job, pos) && job.t_begin < job.t_end) l0 = walk.look(job.t_begin);
+  // bounds over the wave's rows (tokens ascend with the row, positions with the token)
+  const int slot_lo = __builtin_amdgcn_readlane(sight.slot, 0), slot_hi = __builtin_amdgcn_readlane(sight.slot, 31);
+  const int win_hi = __builtin_amdgcn_readlane(sight.win, 31);
+  const int suf_lo = __builtin_amdgcn_readlane(sight.suf, 0), suf_hi = __builtin_amdgcn_readlane(sight.suf, 31);
+
+  f32x16 O[ND];
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) O[d][i] = 0.f;
+  float mx = -INFINITY, l = 0.f, sfx = 0.f;
+
+  // The thread's quarter of a row: wave w brings rows 16 w .. of one page.
+  struct Raw {
+    Quarter k, v;
+    uint32_t ke, ve;
+  };
+  const int in = lane >> 2, quarter = lane & 3;
+  auto load = [&](int t, const Look& lk) __attribute__((always_inline)) {
+    const Rows16 r = rows16(a, job, __builtin_amdgcn_readlane(lk.page, 16 * wave), walk.slot_of(t) + 16 * wave, last_slot, block);
+    const int row = r.row + min(in, r.most);
+    const unsigned at = row * RB + quarter * (RB / 4), ea = ps * RB + row * EB + (D == 128 ? quarter : quarter >> 1);
+    const char *k = (const char*)a.k + r.block, *v = (const char*)a.v + r.block;
+    return Raw{*(const Quarter*)(k + at), *(const Quarter*)(v + at), *(const uint8_t*)(k + ea), *(const uint8_t*)(v + ea)};
+  };
+  const int w_row = 16 * wave + in, w_at = w_row * RBV;
+  auto store = [&](const Raw& raw, int buffer, char* __restrict__ to) __attribute__((always_inline)) {
+    const float uk = fp4_unit(raw.ke);
+    const bool odd = raw.ve > 252;  // counts as 0 in the product; see below
+    const float uv = fp4_unit(odd ? 127 : raw.ve);
+    char* const base = to + buffer * C::kBuffer + w_at;
+#pragma unroll
+    for (int w = 0; w < D / 32; ++w) {
+      const int piece = D / 32 * quarter + w;
+      *(u32x4_t*)(base + 16 * (piece ^ C::turn_k(w_row))) = decode(raw.k[w], uk);
+      *(u32x4_t*)(base + C::kTile + 16 * (piece ^ C::turn_v(w_row))) = decode(odd ? 0 : raw.v[w], uv);
+    }
+    to[C::kFlags + 256 * buffer + 4 * w_row + quarter] = odd;
+  };
+
+  // The lane's first addresses in a tile.
+  const int kx = col * RBV + 16 * (part ^ C::turn_k(col));
+  const int v_row = 4 * part + ((lane & 15) >> 2);
+  const int vx = v_row * RBV + 16 * ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ C::turn_v(v_row)) + 8 * (lane & 1);
+
+  auto scores = [&](const char* from, int k, f32x16& S) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) S[i] = 0.f;
+#pragma unroll
+    for (int u = 0; u < D / 16; ++u) {
+      const u32x4_t x = *(const u32x4_t*)(from + ((k + kx) ^ (32 * u)));
+#pragma unroll
+      for (int i = 0; i < QT; ++i) S = mfma32(x, qf[u][i], S);
+    }
+  };
+  auto top = [&](const f32x16& S) __attribute__((always_inline)) {
+    float t4[4] = {S[0], S[1], S[2], S[3]};
+#pragma unroll
+    for (int i = 4; i < 16; ++i) t4[i & 3] = fmaxf(t4[i & 3], S[i]);
+    const float x = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
+    return fmaxf(x, other_half(x));
+  };
+  auto mask = [&](f32x16& S, int s0, int nb) __attribute__((always_inline)) {
+    const int last = sight.slot - s0 - 32 * nb - 4 * part;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const i32x4 bound = *(const i32x4*)(notes + 32 * nb + 8 * i + 4 * part);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) S[4 * i + j] = bound[j] > sight.win && 8 * i + j <= last ? S[4 * i + j] : -INFINITY;
+    }
+  };
+  auto raise_max = [&](float most) __attribute__((always_inline)) {
+    const float tmax = most * a.scale_log2;
+    const bool raise = tmax > mx + kSlack;
+    if (__any(raise)) {
+      const float f = raise ? __builtin_amdgcn_exp2f(mx - tmax) : 1.f;
+      mx = raise ? tmax : mx;
+      l *= f;
+      sfx *= f;
+#pragma unroll
+      for (int d = 0; d < ND; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) O[d][i] *= f;
+    }
+  };
+  auto weights = [&](f32x16& S) __attribute__((always_inline)) {
+    float s4[4];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      S[i] = __builtin_amdgcn_exp2f(fmaf(S[i], a.scale_log2, mx == -INFINITY ? 0.f : -mx));
+      s4[i & 3] = i < 4 ? S[i] : s4[i & 3] + S[i];
+    }
+    return (s4[0] + s4[1]) + (s4[2] + s4[3]);
+  };
+  auto add_suffix = [&](const f32x16& P, int nb) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const i32x4 p = *(const i32x4*)(notes + 64 + 32 * nb + 8 * i + 4 * part);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) sfx += p[j] > sight.suf ? P[4 * i + j] : 0.f;
+    }
+  };
+  auto product = [&](const char* from, int v, const f32x16& P) __attribute__((always_inline)) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      uint32_t p[4][PT];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) weight_terms<PT>(P[8 * s + 2 * e], P[8 * s + 2 * e + 1], p[e]);
+#pragma unroll
+      for (int d = 0; d < ND; ++d) {
+        const char* at = from + ((v + vx) ^ (64 * d)) + 16 * s * RBV;
+        const u32x2_t x = read_turned(at), y = read_turned(at + 8 * RBV);
+        const u32x4_t z = {x[0], x[1], y[0], y[1]};
+#pragma unroll
+        for (int i = 0; i < PT; ++i) O[d] = mfma32(z, u32x4_t{p[0][i], p[1][i], p[2][i], p[3][i]}, O[d]);
+      }
+    }
+  };
+  // Tile t from its buffer, while the next one's rows go to the other buffer. The two are pointers that do not alias: the
+  // reads need not wait for the writes.
+  auto tile = [&](int t, int buffer, const Raw& raw, const char* __restrict__ from, char* __restrict__ to) __attribute__((always_inline)) {
+    if (t + 1 < job.t_end) store(raw, buffer ^ 1, to);
+    const int s0 = walk.slot_of(t);
+    if (idle || s0 > slot_hi) return;
+    const int tp = is_page(a.map, l0.page) ? l0.pos : kHidden, here = buffer * C::kBuffer;
+    constexpr int kBlock = 32 * RBV;
+    const bool masked = is_masked<NK>(a, tp, s0, slot_lo, win_hi);
+    const int how = suffix_of<NK>(a, tp, suf_lo, suf_hi);
+    if (masked || how == kSome) note(a, notes, tp);
+    const uint32_t flags = *(const uint32_t*)(from + C::kFlags + 256 * buffer + 4 * lane);
+    unsigned long long odd = __ballot(flags != 0);
+    for (; odd != 0; odd &= odd - 1) {  // values that stand for NaN: in their 32 values of the rows that see the slot
+      const int key = __builtin_ctzll(odd);
+      const uint32_t f = __builtin_amdgcn_readlane(flags, key);
+      if (sees(a, sight, s0 + key, __builtin_amdgcn_readlane(tp, key))) {
+#pragma unroll
+        for (int d = 0; d < ND; ++d)
+          if (D == 128 ? f >> (8 * d) & 1 : f >> (16 * d) & 1) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) O[d][i] = NAN;
+          }
+      }
+    }
+    f32x16 S, S1;
+    scores(from, here, S);
+    scores(from, here + kBlock, S1);
+    if (masked) {
+      mask(S, s0, 0);
+      mask(S1, s0, 1);
+    }
+    raise_max(fmaxf(top(S), top(S1)));
+    float sum = weights(S);
+    product(from, here + C::kTile, S);
+    sum += weights(S1);
+    product(from, here + C::kTile + kBlock, S1);
+    l += sum;
+    sfx += how == kAll ? sum : 0.f;
+    if (how == kSome) {
+      add_suffix(S, 0);
+      add_suffix(S1, 1);
+    }
+  };
+  if (job.t_begin < job.t_end) {
+    l1 = walk.look(job.t_begin + 1);
+    Raw raw = load(job.t_begin, l0);
+    store(raw, 0, lds);
+    raw = load(min(job.t_begin + 1, job.t_end - 1), l1);
+    l2 = walk.look(job.t_begin + 2);
+    for (int t = job.t_begin; t < job.t_end; ++t) {
+      __syncthreads();  // every wave has written this tile, and has read the one before
+      const Raw now = raw;
+      if (t + 2 < job.t_end) raw = load(t + 2, l2);
+      const Look l3 = walk.look(t + 3);
+      tile(t, (t - job.t_begin) & 1, now, lds, lds);
+      l0 = l1;
+      l1 = l2;
+      l2 = l3;
+    }
+  }
+  if (idle) return;
+  l += other_half(l);
+  sfx += other_half(sfx);
+  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;  // no slot seen: 0
+  const float mass = l == 0.f ? 0.f : sfx * inv;
+  if (a.ns == 1 && a.conf != nullptr) raise_conf(a.conf + job.b, mass, tok == job.rows / a.G - 1);
+  if (!live) return;
+  if (a.ns > 1) {
+    const size_t at = (size_t)job.split * a.total * a.Hq + qrow;
+#pragma unroll
+    for (int d = 0; d < ND; ++d)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *(f32x4*)(a.po + at * D + 32 * d + 8 * i + 4 * part) = f32x4{O[d][4 * i], O[d][4 * i + 1], O[d][4 * i + 2], O[d][4 * i + 3]};
+    if (part == 0) *(f32x4*)(a.pml + at * 4) = f32x4{mx, l, sfx, 0.f};
+    return;
+  }
+  T* dst = (T*)a.out + qrow * D;
+#pragma unroll
+  for (int d = 0; d < ND; ++d)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float x[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = l == 0.f ? 0.f : O[d][4 * i + e] * inv;
+      if constexpr (sizeof(T) == 4)
+        *(f32x4*)(dst + 32 * d + 8 * i + 4 * part) = f32x4{x[0], x[1], x[2], x[3]};
+      else
+        *(u32x2_t*)(dst + 32 * d + 8 * i + 4 * part) = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+    }
+  if (part == 0) {
+    a.lse[qrow] = l == 0.f ? -INFINITY : kLn2 * (mx + __builtin_amdgcn_logf(l));
+    if (a.suffix != nullptr) a.suffix[qrow] = mass;
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// Launches
+// ------------------------------------------------------------------------------------------
+constexpr int kSideWaves = 4;  // waves for a sequence of few rows beside long chunks
+
+template <int D>
+constexpr int attend_lds() {
+  constexpr int few = kSideWaves * Few<D, 2>::kLds;
+  return Many<D>::kLds > few ? Many<D>::kLds : few;
+}
+
+// Grid: (Hkv, ns, many_tiles + B), flattened with the KV head fastest, the tiles of many rows first.
+template <typename T, int D>
+__global__ __launch_bounds__(kPagedThreads, sizeof(T) == 4 ? 1 : 2) void fp4_attend(PagedAttendArgs a) {
+  __shared__ __align__(512) char lds[attend_lds<D>()];
+  const int per = a.Hkv * a.ns;
+  const int unit = blockIdx.x / per, rest = blockIdx.x % per;
+  Job job;
+  job.h = rest % a.Hkv;
+  job.d0 = 0;
+  const int split = rest / a.Hkv;
+  if (unit < a.many_tiles) {
+    if (!many_job(a, job, unit)) return;
+    job_tiles<kManyKeys>(a, job, kManyRows, split);
+    many_body<T, D>(a, job, lds);
+    return;
+  }
+  if (!few_job(a, job, unit - a.many_tiles, rest == 0)) return;
+  job_tiles<kFewKeys>(a, job, kWaveRows, split);
+  if (job.rows <= 16)
+    few_body<T, D, kSideWaves, D, 1>(a, job, lds);
+  else
+    few_body<T, D, kSideWaves, D, 2>(a, job, lds);
+}
+
+// A step without sequences of more than 32 query rows. DV < D: two workgroups a KV head, each with all of K and half of V,
+// in place of a split of the slots and the launch that joins it.
+// Grid: (Hkv, ns, B) flattened into units; with two halves, groups of 8 units' first halves, then their second.
+template <typename T, int D, int KW, int DV, int NR>
+__global__ __launch_bounds__(64 * KW) void fp4_few(PagedAttendArgs a) {
+  __shared__ __align__(512) char lds[KW * Few<DV, NR>::kLds];
+  const unsigned per = (unsigned)(a.Hkv * a.ns);
+  unsigned unit = blockIdx.x;
+  Job job;
+  job.d0 = 0;
+  if constexpr (DV < D) {
+    const unsigned group = unit / 16 * 8, in = unit % 16, size = min(8u, per * a.map.B - group);
+    unit = group + in % size;
+    job.d0 = in / size * DV;
+  }
+  const unsigned b = unit / per, x = unit % per;
+  job.h = x % a.Hkv;
+  if (!few_job(a, job, b, x == 0 && job.d0 == 0)) return;
+  job_tiles<kFewKeys>(a, job, kWaveRows, x / a.Hkv);
+  few_body<T, D, KW, DV, NR>(a, job, lds);
+}
+
+// ------------------------------------------------------------------------------------------
+// Plan
+// ------------------------------------------------------------------------------------------
+struct Fp4Plan {
+  long many_tiles;  // upper bound over the chunks that `total` rows can be
+  int ns;           // splits of a row's slots
+  int halves;       // workgroups that share a row's output values (fp4_few)
+  bool few;         // fp4_few
+};
+
+constexpr long kFewTarget = 256, kManyTarget = 512;
+constexpr long kHalvesReach = 2560, kHalvesPairs = 64;
+constexpr long kMinSlots = 256, kSplitRows4 = 32;
+constexpr long kMaxSlots = 32768;  // of a split, whatever the number of workgroups
+constexpr long kMaxSplits = 64;
+constexpr long kMaxJoined = (1l << 27) - 8;  // rows that the joining launch has a grid for
+
+static Fp4Plan fp4_plan(const lg_paged_layer& l, const lg_page_map& m, lg_dtype, long total, long max_chunk, long reach) {
+  const long G = l.n_q_heads / l.n_kv_heads;
+  Fp4Plan p;
+  p.many_tiles = 0;
+  p.halves = 1;
+  p.few = max_chunk * G <= kWaveRows;
+  long ns, slots = kMinSlots;
+  if (p.few) {
+    const long units = (long)m.batch * l.n_kv_heads;
+    ns = kFewTarget / units;
+    if (ns > 2 && units >= kHalvesPairs && reach <= kHalvesReach && l.head_dim == 128) ns = 2;
+  } else {
+    if (total * G > kWaveRows) {
+      // a sequence of n rows has at most n / 128 + 1 tiles, and more than 32 rows
+      p.many_tiles = total * G / kManyRows;
+      p.many_tiles += std::min(total * G / (kWaveRows + 1), (long)m.batch);
+    }
+    const long units = (p.many_tiles + m.batch) * l.n_kv_heads;
+    ns = (kManyTarget + units - 1) / units;
+    slots += total * l.n_q_heads / kSplitRows4;
+  }
+  ns = std::min({ns, (reach + slots - 1) / slots, kMaxSplits});
+  const long least = std::min(reach / kMaxSlots, kMaxSplits);
+  if (p.few && ns == 2 && least < 2 && l.head_dim == 128) {
+    ns = 1;
+    p.halves = 2;
+  }
+  p.ns = (int)std::max({ns, least, 1l});
+  if (total * l.n_q_heads > kMaxJoined) p.ns = 1;
+  return p;
+}
+
+static size_t fp4_need(const lg_paged_layer& l, const Fp4Plan& p, long total) {
+  return p.ns > 1 ? (size_t)p.ns * total * l.n_q_heads * (l.head_dim + 4) * 4 : 0;
+}
+
+// Workgroups of the launch (a grid holds fewer than 2^32 threads).
+long fp4_attend_grid(const lg_paged_layer& l, const lg_page_map& m, lg_dtype dtype, int total, int max_chunk) {
+  const Fp4Plan p = fp4_plan(l, m, dtype, total, max_chunk, whole_reach(m));
+  return (p.many_tiles + m.batch) * l.n_kv_heads * p.ns * p.halves;
+}
+
+size_t fp4_attend_need(const lg_paged_layer& l, const lg_page_map& m, lg_dtype dtype, int total, int max_chunk, int window,
+                       int n_sink) {
+  return fp4_need(l, fp4_plan(l, m, dtype, total, max_chunk, window_reach(m, max_chunk, window, n_sink)), total);
+}
+
+// The largest need of any total up to this one and any max_chunk up to this one, with any window (a shorter reach
+// has no more splits). For a given number of splits the need grows with total, and the number falls as total
+// grows, so the ends of its steps count.
+size_t fp4_attend_bytes(const lg_paged_layer& l, const lg_page_map& m, lg_dtype dtype, int total, int max_chunk) {
+  size_t most = 16;
+  for (int form = 0; form < 2; ++form) {
+    const long chunk = form == 0 ? 1 : max_chunk;
+    long t = total;
+    while (t > 0) {
+      const Fp4Plan p = fp4_plan(l, m, dtype, t, chunk, whole_reach(m));
+      most = std::max(most, fp4_need(l, p, t));
+      long lo = 0, hi = t;  // the largest smaller total with more splits
+      while (hi - lo > 1) {
+        const long mid = (lo + hi) / 2;
+        if (fp4_plan(l, m, dtype, mid, chunk, whole_reach(m)).ns > p.ns) lo = mid; else hi = mid;
+      }
+      t = lo;
+    }
+  }
+  return align_up(most, 16);
+}
+
+template <typename T, int D, int KW, int NR>
+static void launch_few(const PagedAttendArgs& a, const Fp4Plan& p, dim3 grid, hipStream_t st) {
+  if (p.halves == 1)
+    hipLaunchKernelGGL((fp4_few<T, D, KW, D, NR>), grid, dim3(64 * KW), 0, st, a);
+  else if constexpr (D == 128)
+    hipLaunchKernelGGL((fp4_few<T, D, KW, D / 2, NR>), grid, dim3(64 * KW), 0, st, a);
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(kRowThreads) void fp4_attend(Fp4AttendArgs a) {
-  __shared__ float q[D];
-  const int lane = threadIdx.x, r = blockIdx.x / a.Hq, hq = blockIdx.x % a.Hq, h = hq / a.G;
-  const int b = seq_of_row(a.q_start, a.map.B, r);
-  if (b >= a.map.B) return;
-  const Chunk c = chunk_of(a.q_start, b, a.total);
-  if (r < c.first || r >= c.first + c.n) return;
-  const int base = a.base[b];
-  if (base < 0 || c.n > a.max_chunk || base > a.map.cap - c.n) {
-    if (a.conf != nullptr && lane == 0) a.conf[b] = NAN;
-    return;
-  }
-  const MapArgs& m = a.map;
-  const int slot_q = base + r - c.first;
-  const int32_t* pos = m.pos + (size_t)b * m.cap;
-  const int p_q = pos[slot_q];
-  const int win = a.window > 0 ? (int)max((long long)p_q - a.window, (long long)INT32_MIN) : INT32_MIN;
-  const int suf = (int)max((long long)p_q - (a.suffix_w != nullptr ? max(a.suffix_w[b], 0) : 0), (long long)INT32_MIN);
-  const size_t row = (size_t)r * a.Hq + hq;
-  for (int d = lane; d < D; d += 64) q[d] = (float)((const T*)a.q)[row * D + d];
-  __syncthreads();
-  const size_t block = fp4_block(D, m.shift);
-  const int ps = 1 << m.shift;
-  float mx = -INFINITY, l = 0.f, sfx = 0.f, o[2] = {0.f, 0.f};
-  for (int s0 = 0; s0 <= slot_q; s0 += 64) {
-    const int s = s0 + lane;
-    int page = -1;
-    float sc = -INFINITY;
-    bool see = false, near = false;
-    if (s <= slot_q) {
-      page = m.table[(size_t)b * m.P + (s >> m.shift)];
-      see = is_page(m, page) && (a.window == 0 || pos[s] > win || pos[s] < a.n_sink);
-      near = pos[s] > suf;
-    }
-    if (see) {
-      const char* at = a.k + ((size_t)page * a.Hkv + h) * block;
-      const uint32_t* codes = (const uint32_t*)(at + (s & (ps - 1)) * (D / 2));
-      sc = 0.f;
-      for (int w = 0; w < D / 8; ++w) {
-        const float u = fp4_unit(*(const uint8_t*)(at + ps * (D / 2) + (s & (ps - 1)) * (D / 32) + w / 4));
-        const f32x2 x0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[w], u, 0), x1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[w], u, 1);
-        const f32x2 x2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[w], u, 2), x3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(codes[w], u, 3);
-        sc += x0[0] * q[8 * w] + x0[1] * q[8 * w + 1] + x1[0] * q[8 * w + 2] + x1[1] * q[8 * w + 3] + x2[0] * q[8 * w + 4] +
-              x2[1] * q[8 * w + 5] + x3[0] * q[8 * w + 6] + x3[1] * q[8 * w + 7];
-      }
-      sc *= a.scale_log2;
-    }
-    const float top = fmaxf(mx, wave_max(sc)), ms = top == -INFINITY ? 0.f : top;
-    const float f = __builtin_amdgcn_exp2f(mx - ms), p = see ? __builtin_amdgcn_exp2f(sc - ms) : 0.f;
-    mx = top;
-    l = l * f + wave_sum(p);
-    sfx = sfx * f + wave_sum(near ? p : 0.f);
-    o[0] *= f;
-    o[1] *= f;
-    unsigned long long seen = __ballot(see);
-    while (seen != 0) {
-      const int j = __builtin_ctzll(seen);
-      seen &= seen - 1;
-      const float pj = __shfl(p, j, 64);
-      const int pg = __shfl(page, j, 64), in = (s0 + j) & (ps - 1), d = lane * (D / 64);
-      const char* at = a.v + ((size_t)pg * a.Hkv + h) * block;
-      const float u = fp4_unit(*(const uint8_t*)(at + ps * (D / 2) + in * (D / 32) + d / 32));
-      const f32x2 x = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4((uint32_t)*(const uint8_t*)(at + in * (D / 2) + d / 2), u, 0);
-      if constexpr (D == 128) {
-        o[0] += pj * x[0];
-        o[1] += pj * x[1];
-      } else {
-        o[0] += pj * x[d & 1];
-      }
-    }
-  }
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  for (int i = 0; i < D / 64; ++i) ((T*)a.out)[row * D + lane * (D / 64) + i] = (T)(l == 0.f ? 0.f : o[i] * inv);
-  if (lane == 0) {
-    const float mass = l == 0.f ? 0.f : sfx * inv;
-    a.lse[row] = l == 0.f ? -INFINITY : kLn2 * (mx + __builtin_amdgcn_logf(l));
-    if (a.suffix != nullptr) a.suffix[row] = mass;
-    if (a.conf != nullptr && r == c.first + c.n - 1) atomicMax((int*)a.conf + b, mass != mass ? 0x7fc00000 : __float_as_int(mass));
-  }
+static void launch_typed(const PagedAttendArgs& a, const Fp4Plan& p, dim3 grid, hipStream_t st) {
+  constexpr int KW = 8;
+  if (!p.few)
+    hipLaunchKernelGGL((fp4_attend<T, D>), grid, dim3(kPagedThreads), 0, st, a);
+  else if ((long)a.max_chunk * a.G <= 16)
+    launch_few<T, D, KW, 1>(a, p, grid, st);
+  else
+    launch_few<T, D, KW, 2>(a, p, grid, st);
+  if (p.ns > 1) launch_paged_join(a, sizeof(T) == 2, D, st);
 }
-
-long fp4_attend_grid(const lg_paged_layer& l, const lg_page_map&, lg_dtype, int total, int) { return (long)total * l.n_q_heads / 8; }
-size_t fp4_attend_need(const lg_paged_layer&, const lg_page_map&, lg_dtype, int, int, int, int) { return 0; }
-size_t fp4_attend_bytes(const lg_paged_layer&, const lg_page_map&, lg_dtype, int, int) { return 16; }
 
 hipError_t launch_fp4_attend(const lg_paged_layer& l, const lg_page_map& m, lg_dtype dtype, const void* q, void* out,
                              const int32_t* q_start, const int32_t* base, int total, int max_chunk, int window,
                              int n_sink, const int32_t* suffix_w, float* lse, float* suffix, float* conf, void* ws,
                              hipStream_t st) {
-  Fp4AttendArgs a = {};
+  const Fp4Plan p = fp4_plan(l, m, dtype, total, max_chunk, window_reach(m, max_chunk, window, n_sink));
+  PagedAttendArgs a = {};
   a.q = q;
-  a.k = (const char*)l.k;
-  a.v = (const char*)l.v;
+  a.k = l.k;
+  a.v = l.v;
   a.out = out;
   a.q_start = q_start;
   a.base = base;
@@ -131,23 +931,26 @@ hipError_t launch_fp4_attend(const lg_paged_layer& l, const lg_page_map& m, lg_d
   a.lse = lse;
   a.suffix = suffix;
   a.conf = conf;
+  a.po = (float*)ws;
+  a.pml = (float*)ws + (size_t)p.ns * total * l.n_q_heads * l.head_dim;
   a.map = map_args(m);
   a.Hq = l.n_q_heads;
   a.Hkv = l.n_kv_heads;
   a.G = l.n_q_heads / l.n_kv_heads;
-  a.D = l.head_dim;
   a.total = total;
   a.max_chunk = max_chunk;
   a.window = window;
   a.n_sink = n_sink;
+  a.ns = p.ns;
+  a.many_tiles = (int)p.many_tiles;
   a.scale_log2 = kLog2e / sqrtf((float)l.head_dim);
-  const dim3 grid((unsigned)total * l.n_q_heads), block(kRowThreads);
+  const dim3 grid((unsigned)((p.many_tiles + m.batch) * l.n_kv_heads * p.ns * p.halves));
   if (dtype == LG_BF16) {
-    if (l.head_dim == 128) hipLaunchKernelGGL((fp4_attend<__bf16, 128>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((fp4_attend<__bf16, 64>), grid, block, 0, st, a);
+    if (l.head_dim == 128) launch_typed<__bf16, 128>(a, p, grid, st);
+    else launch_typed<__bf16, 64>(a, p, grid, st);
   } else {
-    if (l.head_dim == 128) hipLaunchKernelGGL((fp4_attend<float, 128>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((fp4_attend<float, 64>), grid, block, 0, st, a);
+    if (l.head_dim == 128) launch_typed<float, 128>(a, p, grid, st);
+    else launch_typed<float, 64>(a, p, grid, st);
   }
   return hipGetLastError();
 }
