@@ -35,21 +35,30 @@ __device__ __forceinline__ void weight_terms(float x, float y, uint32_t (&t)[N])
   }
 }
 
-// 8 values of a query as N terms. float32: cut off after 8 and 16 bits, so that no term is larger than the value; one that
-// is not finite is its first term alone.
+// 8 values of a query as they lie, and as N terms. float32: cut off after 8 and 16 bits, so that no term is larger than the
+// value; one that is not finite is its first term alone.
+template <typename T>
+struct Eight {
+  u32x4_t x[sizeof(T) / 2];
+};
+template <typename T>
+__device__ __forceinline__ Eight<T> load_eight(const T* src) {
+  Eight<T> y;
+  y.x[0] = *(const u32x4_t*)src;
+  if constexpr (sizeof(T) == 4) y.x[1] = *(const u32x4_t*)(src + 4);
+  return y;
+}
 template <typename T, int N>
-__device__ __forceinline__ void load_query(const T* src, u32x4_t (&t)[N]) {
+__device__ __forceinline__ void query_terms(const Eight<T>& q, u32x4_t (&t)[N]) {
   if constexpr (N == 1) {
-    t[0] = *(const u32x4_t*)src;
+    t[0] = q.x[0];
   } else {
-    const f32x4 a = *(const f32x4*)src, b = *(const f32x4*)(src + 4);
-    const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       uint32_t w[N] = {};
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float y = x[2 * i + e];
+        float y = __uint_as_float(q.x[i / 2][2 * (i % 2) + e]);
         const bool finite = (__float_as_uint(y) & 0x7f800000u) != 0x7f800000u;
         if (!finite) {
           w[0] |= (pack_bf16(y, y) & 0xffffu) << (16 * e);
@@ -88,42 +97,58 @@ __device__ __forceinline__ u32x2_t read_turned(const char* at) {
   return __builtin_bit_cast(u32x2_t, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) i16x4*)at));
 }
 
+// The larger one, NaN if one is (a row with such a score is NaN whatever its maximum), which takes no instruction to make
+// its operands canonical.
+__device__ __forceinline__ float larger(float x, float y) { return __builtin_elementwise_maximum(x, y); }
+
 // ------------------------------------------------------------------------------------------
 // Tiles
 // ------------------------------------------------------------------------------------------
+// A value at an offset of at most 32 bits in bytes: the base stays in scalar registers.
+template <typename X>
+__device__ __forceinline__ X at32(const X* base, unsigned off) { return *(const X*)((const char*)base + off); }
+
 struct Look {
-  int page, pos;  // of the lane's slot
+  int page, pos;
 };
 
-// The rows of a tile that a workgroup or wave works on, as slots.
+// An entry, by way of the scalar cache, of an array that nothing writes while the kernel reads it.
+__device__ __forceinline__ int of_all(const int32_t* x, int at) {
+  return ((const __attribute__((address_space(4))) int32_t*)x)[__builtin_amdgcn_readfirstlane(at)];
+}
+
+// The slots of a workgroup's rows in tiles of NK.
 template <int NK>
 struct Walk {
   const PagedAttendArgs& a;
   const Job& job;
   const int32_t *table, *pos;
-  int last_slot;  // the last one that any of the rows sees
+  int last_slot;  // the last one that any of the rows sees; what is read of slots behind it is read of this one
 
   __device__ __forceinline__ int slot_of(int t) const { return (t < job.sink_tiles ? t : t - job.sink_tiles + job.tile0) * NK; }
-  // Columns and positions of a tile, a lane a slot; slots behind last_slot read as last_slot: no row sees them.
+  // The page of a slot that all lanes ask for: scalar loads are counted apart from the rows', which return in order, so it
+  // is there before the rows that were asked for first.
+  __device__ __forceinline__ int page_of(int slot) const { return of_all(table, min(slot, last_slot) >> a.map.shift); }
+  // Page and position of the lane's slot of a tile.
   __device__ __forceinline__ Look look(int t) const {
-    const int s = min(slot_of(min(t, job.t_end - 1)) + ((int)threadIdx.x & (NK - 1)), last_slot);
-    return {table[s >> a.map.shift], pos[s]};
+    const unsigned s = min(slot_of(min(t, job.t_end - 1)) + ((int)threadIdx.x & (NK - 1)), last_slot);  // below 2^30
+    return {at32(table, 4 * (s >> a.map.shift)), at32(pos, 4 * s)};
+  }
+  __device__ __forceinline__ int pos_of_lane(int s0) const {  // slots are below 2^30
+    return at32(pos, 4u * (unsigned)min(s0 + ((int)threadIdx.x & (NK - 1)), last_slot));
   }
 };
 
-// 16 rows of one page: where their block begins, the first row in it, and the rows that there are behind that.
-struct Rows16 {
-  size_t block;
-  int row, most;
+// Where row `row` of a page and its exponents lie in K or V (a page that is none: page 0). Blocks have at least 544
+// bytes, so their numbers stay below 2^32 in any memory.
+struct Block {
+  size_t rows, exps;
 };
-__device__ __forceinline__ Rows16 rows16(const PagedAttendArgs& a, const Job& job, int page, int slot, int last_slot, size_t block) {
-  Rows16 r;
-  page = is_page(a.map, page) ? page : 0;
-  slot = min(slot, last_slot & ~15);
-  r.block = ((size_t)page * a.Hkv + job.h) * block;
-  r.row = slot & ((1 << a.map.shift) - 1);
-  r.most = last_slot - slot;
-  return r;
+template <int D>
+__device__ __forceinline__ Block block_at(const PagedAttendArgs& a, const Job& job, int page, int row) {
+  const unsigned n = (unsigned)(is_page(a.map, page) ? page : 0) * (unsigned)a.Hkv + (unsigned)job.h;
+  const size_t at = (size_t)n * fp4_block(D, a.map.shift);
+  return {at + (long)row * (D / 2), at + ((size_t)(D / 2) << a.map.shift) + (long)row * (D / 32)};
 }
 
 // What a row of the wave sees: slots up to its own, at positions above win or below n_sink; it counts those above
@@ -131,10 +156,9 @@ __device__ __forceinline__ Rows16 rows16(const PagedAttendArgs& a, const Job& jo
 struct Sight {
   int slot, win, suf;
 };
-__device__ __forceinline__ Sight sight_of(const PagedAttendArgs& a, const Job& job, const int32_t* pos, int tok) {
+__device__ __forceinline__ Sight sight_of(const PagedAttendArgs& a, int slot, int p, int sw) {
   Sight s;
-  s.slot = job.base + tok;
-  const int p = pos[s.slot], sw = a.suffix_w != nullptr ? a.suffix_w[job.b] : 0;
+  s.slot = slot;
   s.win = a.window > 0 ? (int)max((long long)p - a.window, (long long)INT32_MIN) : INT32_MIN;
   s.suf = (int)max((long long)p - max(sw, 0), (long long)INT32_MIN);
   return s;
@@ -195,8 +219,9 @@ struct Few {
 template <typename T, int D, int KW, int DV, int NR>
 __device__ __forceinline__ void few_body(const PagedAttendArgs& a, Job job, char* lds) {
   using C = Few<DV, NR>;
+  constexpr int NK = kFewKeys;
   constexpr int QT = q_terms<T>(), PT = p_terms<T, true>();
-  constexpr int NK = kFewKeys, NJ = NK / 16, NKK = D / 32, ND = DV / 16;
+  constexpr int NJ = NK / 16, NKK = D / 32, ND = DV / 16;
   constexpr int RB = D / 2, EB = D / 32;    // bytes of a row and of its exponents
   constexpr int VP = DV / 32, VU = NK * VP / 64;  // groups of a row of V, and of them a lane's
   constexpr int RBV = 2 * DV;
@@ -205,33 +230,16 @@ __device__ __forceinline__ void few_body(const PagedAttendArgs& a, Job job, char
   const int part = lane >> 4, col = lane & 15;
   char* const my = lds + wave * C::kLds;
   int32_t* const notes = (int32_t*)(my + C::kTile);
-  const size_t block = fp4_block(D, a.map.shift);
   const int ps = 1 << a.map.shift;
-  Walk<NK> walk = {a, job, a.map.table + (size_t)job.b * a.map.P, a.map.pos + (size_t)job.b * a.map.cap,
-                   job.base + (job.rows - 1) / a.G};
+  const Walk<NK> walk = {a, job, a.map.table + (size_t)job.b * a.map.P, a.map.pos + (size_t)job.b * a.map.cap,
+                         job.base + (job.rows - 1) / a.G};
   const int32_t* const pos = walk.pos;
   const int last_slot = walk.last_slot;
 
-  int t_first = job.t_begin + wave;
-  Look l0 = {}, l1 = {};
-  if (t_first < job.t_end) l0 = walk.look(t_first);
-  u32x4_t qf[NR][NKK][QT];
-  Sight sight[NR];
-#pragma unroll
-  for (int n = 0; n < NR; ++n) {
-    const int R = min(16 * n + col, job.rows - 1), tok = R / a.G;  // rows behind the last repeat it; they are not written
-    const T* src = (const T*)a.q + ((size_t)(job.first + tok) * a.Hq + job.h * a.G + R - tok * a.G) * D + part * (D / 4);
-#pragma unroll
-    for (int k = 0; k < NKK; ++k) load_query<T, QT>(src + 8 * k, qf[n][k]);
-    sight[n] = sight_of(a, job, pos, tok);
-  }
-  if (skip_hidden<NK>(a, job, pos)) {
-    t_first = job.t_begin + wave;
-    if (t_first < job.t_end) l0 = walk.look(t_first);
-  }
-  // the first and the last row's
-  const Sight lo = sight_of(a, job, pos, 0), hi = sight_of(a, job, pos, (job.rows - 1) / a.G);
-
+  // What the first rows need comes first; everything else is asked for behind it and used when they are on their way.
+  skip_hidden<NK>(a, job, pos);
+  const int t_first = job.t_begin + wave;
+  const bool some = t_first < job.t_end;
   f32x4 O[NR][ND];
   float mx[NR], l[NR], sfx[NR];  // l and sfx: the lane's share of the keys
 #pragma unroll
@@ -242,52 +250,99 @@ __device__ __forceinline__ void few_body(const PagedAttendArgs& a, Job job, char
     l[n] = sfx[n] = 0.f;
   }
 
+  // The pages of a tile: of its first 16 slots, and where a page is 16 slots of the others.
+  struct Pages {
+    int first, second;
+  };
+  const bool short_pages = ps == 16;
+  auto pages_of = [&](int t) __attribute__((always_inline)) {
+    const int s0 = walk.slot_of(min(t, job.t_end - 1));
+    Pages p = {walk.page_of(s0), 0};
+    if (short_pages) p.second = walk.page_of(s0 + 16);
+    return p;
+  };
+  // A tile as it lies in memory, the lane's pieces with their exponents.
   struct Raw {
     KRow k[NJ];
     u32x4_t v[VU];
     uint32_t ke[NJ], ve[VU];
+    int pos;
+    Pages pages;
   };
-  auto load = [&](int t, const Look& lk) __attribute__((always_inline)) {
+  // Rows behind last_slot are read as that one.
+  auto load = [&](int t, const Pages& p) __attribute__((always_inline)) {
     Raw raw;
-    Rows16 r[NJ];
-    const int s0 = walk.slot_of(t);
+    const int s0 = walk.slot_of(t), most = last_slot - s0;
+    const Block first = block_at<D>(a, job, p.first, s0 & (ps - 1));
+    // as if the second page began 16 rows earlier
+    const Block second = short_pages && most >= 16 ? block_at<D>(a, job, p.second, -16) : first;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      r[j] = rows16(a, job, __builtin_amdgcn_readlane(lk.page, 16 * j), s0 + 16 * j, last_slot, block);
-      const int row = r[j].row + min(col, r[j].most);
-      const char* at = (const char*)a.k + r[j].block;
-      raw.k[j] = *(const KRow*)(at + row * RB + part * (RB / 4));
-      raw.ke[j] = *(const uint8_t*)(at + ps * RB + row * EB + (D == 128 ? part : part >> 1));
+      const unsigned row = min(16 * j + col, most);
+      raw.k[j] = at32((const KRow*)((const char*)a.k + (j == 0 ? first : second).rows), row * RB + part * (RB / 4));
+      raw.ke[j] = at32((const uint8_t*)a.k + (j == 0 ? first : second).exps, row * EB + (D == 128 ? part : part >> 1));
     }
 #pragma unroll
     for (int u = 0; u < VU; ++u) {
-      const int in = lane / VP + u * (64 / VP);  // row of the tile
-      const bool second = VP == 4 ? u & 1 : in >= 16;
-      const size_t first = second ? r[1].block : r[0].block;
-      const int row = (second ? r[1].row : r[0].row) + min(in & 15, second ? r[1].most : r[0].most);
-      const char* at = (const char*)a.v + first;
-      raw.v[u] = *(const u32x4_t*)(at + row * RB + job.d0 / 2 + lane % VP * 16);
-      raw.ve[u] = *(const uint8_t*)(at + ps * RB + row * EB + job.d0 / 32 + lane % VP);
+      const unsigned row = min(lane / VP + u * (64 / VP), most);
+      const bool later = VP == 4 ? u == 1 : lane >= 32;
+      raw.v[u] = at32((const u32x4_t*)((const char*)a.v + job.d0 / 2 + (later ? second : first).rows), row * RB + lane % VP * 16);
+      raw.ve[u] = at32((const uint8_t*)a.v + job.d0 / 32 + (later ? second : first).exps, row * EB + lane % VP);
     }
+    raw.pos = walk.pos_of_lane(s0);
+    raw.pages = p;
     return raw;
   };
+  Pages next = {};
+  Raw raw = {};
+  if (some) next = pages_of(t_first);
+  Eight<T> query[NR][NKK];
+  int slot_q[NR], p_q[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+    const int R = min(16 * n + col, job.rows - 1), tok = R / a.G;  // rows behind the last repeat it; they are not written
+    const T* src = (const T*)a.q + ((size_t)(job.first + tok) * a.Hq + job.h * a.G + R - tok * a.G) * D + part * (D / 4);
+#pragma unroll
+    for (int k = 0; k < NKK; ++k) query[n][k] = load_eight(src + 8 * k);
+    slot_q[n] = job.base + tok;
+    p_q[n] = pos[slot_q[n]];
+  }
+  const int p_lo = of_all(pos, job.base), p_hi = of_all(pos, last_slot);
+  const int sw = of_all(a.suffix_w != nullptr ? a.suffix_w : a.base, job.b);  // without suffix_w nothing goes by it
+  if (some) {
+    raw = load(t_first, next);
+    if (t_first + KW < job.t_end) next = pages_of(t_first + KW);
+  }
+  u32x4_t qf[NR][NKK][QT];
+  Sight sight[NR];
+#pragma unroll
+  for (int n = 0; n < NR; ++n) {
+#pragma unroll
+    for (int k = 0; k < NKK; ++k) query_terms<T, QT>(query[n][k], qf[n][k]);
+    sight[n] = sight_of(a, slot_q[n], p_q[n], sw);
+  }
+  // the first and the last row's
+  const Sight lo = sight_of(a, job.base, p_lo, sw), hi = sight_of(a, last_slot, p_hi, sw);
 
   const int v_row = lane / VP, v_write = v_row * RBV, v_turn = C::turn(v_row);
   const int k_row = 4 * part + (col >> 2);
   const char* const v_read = my + k_row * RBV + 16 * (((col & 3) >> 1) ^ C::turn(k_row)) + 8 * (col & 1);
 
-  auto tile = [&](int t, const Look& lk, const Raw& raw) __attribute__((always_inline)) {
-    const int s0 = walk.slot_of(t);
-    const int tp = is_page(a.map, lk.page) ? lk.pos : kHidden;
+  // A tile up to its scores, which is when its rows are not needed any more.
+  f32x4 S[NR][NJ];
+  int s0, tp;
+  auto begin = [&](int t, const Raw& raw) __attribute__((always_inline)) {
+    s0 = walk.slot_of(t);
+    tp = is_page(a.map, short_pages && (lane & 16) != 0 ? raw.pages.second : raw.pages.first) ? raw.pos : kHidden;
     // V as bfloat16
 #pragma unroll
     for (int u = 0; u < VU; ++u) {
       u32x4_t codes = raw.v[u];
-      const unsigned long long odd = __ballot(raw.ve[u] > 252);
-      if (odd != 0) {
+      const bool nan = raw.ve[u] > 252;
+      if (__any(nan)) {
         // Groups that stand for NaN: 0 in the product, and NaN in their 32 values of the rows that see the slot.
-        if (raw.ve[u] > 252) codes = u32x4_t{0, 0, 0, 0};
-        for (unsigned long long left = odd; left != 0; left &= left - 1) {
+        if (nan) codes = u32x4_t{0, 0, 0, 0};
+        for (unsigned long long left = __ballot(nan); left != 0; left &= left - 1) {
           const int bit = __builtin_ctzll(left), key = bit / VP + u * (64 / VP), g = bit % VP;
           const int p = __builtin_amdgcn_readlane(tp, key);
 #pragma unroll
@@ -299,12 +354,11 @@ __device__ __forceinline__ void few_body(const PagedAttendArgs& a, Job job, char
           }
         }
       }
-      const float unit = fp4_unit(raw.ve[u] > 252 ? 127 : raw.ve[u]);
+      const float unit = fp4_unit(nan ? 127 : raw.ve[u]);
 #pragma unroll
       for (int w = 0; w < 4; ++w)
         *(u32x4_t*)(my + u * (64 / VP) * RBV + v_write + 16 * ((4 * (lane % VP) + w) ^ v_turn)) = decode(codes[w], unit);
     }
-    f32x4 S[NR][NJ];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
       const float unit = fp4_unit(raw.ke[j]);
@@ -319,6 +373,8 @@ __device__ __forceinline__ void few_body(const PagedAttendArgs& a, Job job, char
           for (int i = 0; i < QT; ++i) S[n][j] = mfma16(x, qf[n][k][i], S[n][j]);
       }
     }
+  };
+  auto finish = [&]() __attribute__((always_inline)) {
     const bool masked = is_masked<NK>(a, tp, s0, lo.slot, hi.win);
     const int how = suffix_of<NK>(a, tp, lo.suf, hi.suf);
     if (masked || how == kSome) note(a, notes, tp);
@@ -337,11 +393,11 @@ __device__ __forceinline__ void few_body(const PagedAttendArgs& a, Job job, char
     uint32_t P[NR][NK / 32][4][PT];
 #pragma unroll
     for (int n = 0; n < NR; ++n) {
-      float top = fmaxf(fmaxf(S[n][0][0], S[n][0][1]), fmaxf(S[n][0][2], S[n][0][3]));
+      float top = larger(larger(S[n][0][0], S[n][0][1]), larger(S[n][0][2], S[n][0][3]));
 #pragma unroll
-      for (int j = 1; j < NJ; ++j) top = fmaxf(top, fmaxf(fmaxf(S[n][j][0], S[n][j][1]), fmaxf(S[n][j][2], S[n][j][3])));
-      top = fmaxf(top, other_row(top));
-      top = fmaxf(top, other_half(top)) * a.scale_log2;
+      for (int j = 1; j < NJ; ++j) top = larger(larger(top, S[n][j][0]), larger(larger(S[n][j][1], S[n][j][2]), S[n][j][3]));
+      top = larger(top, other_row(top));
+      top = larger(top, other_half(top)) * a.scale_log2;
       // The running maximum follows only when a score passes it by kSlack (weights are then at most 2^kSlack).
       const bool raise = top > mx[n] + kSlack;
       if (__any(raise)) {
@@ -389,22 +445,16 @@ __device__ __forceinline__ void few_body(const PagedAttendArgs& a, Job job, char
       }
   };
 
-  if (t_first < job.t_end) {
-    l1 = walk.look(t_first + KW);
-    Raw raw = load(t_first, l0);
-    for (int t = t_first; t < job.t_end; t += KW) {
-      Raw next = raw;
-      if (t + KW < job.t_end) next = load(t + KW, l1);
-      const Look l2 = walk.look(t + 2 * KW);
-      tile(t, l0, raw);
-      raw = next;
-      l0 = l1;
-      l1 = l2;
-    }
+  for (int t = t_first; t < job.t_end; t += KW) {
+    begin(t, raw);
+    if (t + KW < job.t_end) raw = load(t + KW, next);
+    if (t + 2 * KW < job.t_end) next = pages_of(t + 2 * KW);
+    finish();
   }
 
   // Join the waves: their numerators and statistics through LDS.
-  constexpr int kRows = 16 * NR, kParts = 64 * KW / kRows, kPairs = DV / (2 * kParts);
+  constexpr int kRows = 16 * NR, kShare = 64 * KW / kRows, kParts = kShare < DV / 2 ? kShare : DV / 2;  // threads a row
+  constexpr int kPairs = DV / (2 * kParts);
   float* const num = (float*)my;
 #pragma unroll
   for (int n = 0; n < NR; ++n) {
@@ -518,10 +568,9 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int part = lane >> 5, col = lane & 31;
   int32_t* const notes = (int32_t*)(lds + C::kOwnNotes + wave * kNotes);
-  const size_t block = fp4_block(D, a.map.shift);
   const int ps = 1 << a.map.shift;
-  Walk<NK> walk = {a, job, a.map.table + (size_t)job.b * a.map.P, a.map.pos + (size_t)job.b * a.map.cap,
-                   job.base + (min(job.row0 + kManyRows, job.rows) - 1) / a.G};
+  const Walk<NK> walk = {a, job, a.map.table + (size_t)job.b * a.map.P, a.map.pos + (size_t)job.b * a.map.cap,
+                         job.base + (min(job.row0 + kManyRows, job.rows) - 1) / a.G};
   const int32_t* const pos = walk.pos;
   const int last_slot = walk.last_slot;
 
@@ -530,13 +579,11 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
   const bool live = R < job.rows, idle = wrow0 >= job.rows;  // a wave without rows only loads
   const int Rc = live ? R : job.rows - 1, tok = Rc / a.G;    // rows behind the last repeat it; they are not written
   const size_t qrow = (size_t)(job.first + tok) * a.Hq + job.h * a.G + Rc - tok * a.G;
-  Look l0 = {}, l1 = {}, l2 = {};
-  if (job.t_begin < job.t_end) l0 = walk.look(job.t_begin);
   u32x4_t qf[D / 16][QT];
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k) load_query<T, QT>((const T*)a.q + qrow * D + 16 * k + 8 * part, qf[k]);
-  const Sight sight = sight_of(a, job, pos, tok);
-  if (skip_hidden<NK>(a, job, pos) && job.t_begin < job.t_end) l0 = walk.look(job.t_begin);
+  for (int k = 0; k < D / 16; ++k) query_terms<T, QT>(load_eight((const T*)a.q + qrow * D + 16 * k + 8 * part), qf[k]);
+  const Sight sight = sight_of(a, job.base + tok, pos[job.base + tok], a.suffix_w != nullptr ? a.suffix_w[job.b] : 0);
+  skip_hidden<NK>(a, job, pos);
   // bounds over the wave's rows (tokens ascend with the row, positions with the token)
   const int slot_lo = __builtin_amdgcn_readlane(sight.slot, 0), slot_hi = __builtin_amdgcn_readlane(sight.slot, 31);
   const int win_hi = __builtin_amdgcn_readlane(sight.win, 31);
@@ -556,11 +603,12 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
   };
   const int in = lane >> 2, quarter = lane & 3;
   auto load = [&](int t, const Look& lk) __attribute__((always_inline)) {
-    const Rows16 r = rows16(a, job, __builtin_amdgcn_readlane(lk.page, 16 * wave), walk.slot_of(t) + 16 * wave, last_slot, block);
-    const int row = r.row + min(in, r.most);
-    const unsigned at = row * RB + quarter * (RB / 4), ea = ps * RB + row * EB + (D == 128 ? quarter : quarter >> 1);
-    const char *k = (const char*)a.k + r.block, *v = (const char*)a.v + r.block;
-    return Raw{*(const Quarter*)(k + at), *(const Quarter*)(v + at), *(const uint8_t*)(k + ea), *(const uint8_t*)(v + ea)};
+    const int s0 = min(walk.slot_of(t) + 16 * wave, last_slot & ~15);  // rows behind last_slot repeat it
+    const Block at = block_at<D>(a, job, __builtin_amdgcn_readlane(lk.page, 16 * wave), s0 & (ps - 1));
+    const unsigned row = min(in, last_slot - s0);
+    const unsigned off = row * RB + quarter * (RB / 4), ea = row * EB + (D == 128 ? quarter : quarter >> 1);
+    return Raw{at32((const Quarter*)((const char*)a.k + at.rows), off), at32((const Quarter*)((const char*)a.v + at.rows), off),
+               at32((const uint8_t*)a.k + at.exps, ea), at32((const uint8_t*)a.v + at.exps, ea)};
   };
   const int w_row = 16 * wave + in, w_at = w_row * RBV;
   auto store = [&](const Raw& raw, int buffer, char* __restrict__ to) __attribute__((always_inline)) {
@@ -595,9 +643,9 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
   auto top = [&](const f32x16& S) __attribute__((always_inline)) {
     float t4[4] = {S[0], S[1], S[2], S[3]};
 #pragma unroll
-    for (int i = 4; i < 16; ++i) t4[i & 3] = fmaxf(t4[i & 3], S[i]);
-    const float x = fmaxf(fmaxf(t4[0], t4[1]), fmaxf(t4[2], t4[3]));
-    return fmaxf(x, other_half(x));
+    for (int i = 4; i < 16; ++i) t4[i & 3] = larger(t4[i & 3], S[i]);
+    const float x = larger(larger(t4[0], t4[1]), larger(t4[2], t4[3]));
+    return larger(x, other_half(x));
   };
   auto mask = [&](f32x16& S, int s0, int nb) __attribute__((always_inline)) {
     const int last = sight.slot - s0 - 32 * nb - 4 * part;
@@ -657,11 +705,11 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
   };
   // Tile t from its buffer, while the next one's rows go to the other buffer. The two are pointers that do not alias: the
   // reads need not wait for the writes.
-  auto tile = [&](int t, int buffer, const Raw& raw, const char* __restrict__ from, char* __restrict__ to) __attribute__((always_inline)) {
+  auto tile = [&](int t, int buffer, int tp, const Raw& raw, const char* __restrict__ from, char* __restrict__ to) __attribute__((always_inline)) {
     if (t + 1 < job.t_end) store(raw, buffer ^ 1, to);
     const int s0 = walk.slot_of(t);
     if (idle || s0 > slot_hi) return;
-    const int tp = is_page(a.map, l0.page) ? l0.pos : kHidden, here = buffer * C::kBuffer;
+    const int here = buffer * C::kBuffer;
     constexpr int kBlock = 32 * RBV;
     const bool masked = is_masked<NK>(a, tp, s0, slot_lo, win_hi);
     const int how = suffix_of<NK>(a, tp, suf_lo, suf_hi);
@@ -687,7 +735,7 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
       mask(S, s0, 0);
       mask(S1, s0, 1);
     }
-    raise_max(fmaxf(top(S), top(S1)));
+    raise_max(larger(top(S), top(S1)));
     float sum = weights(S);
     product(from, here + C::kTile, S);
     sum += weights(S1);
@@ -700,17 +748,17 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
     }
   };
   if (job.t_begin < job.t_end) {
-    l1 = walk.look(job.t_begin + 1);
+    Look l0 = walk.look(job.t_begin), l1 = walk.look(job.t_begin + 1);
     Raw raw = load(job.t_begin, l0);
     store(raw, 0, lds);
     raw = load(min(job.t_begin + 1, job.t_end - 1), l1);
-    l2 = walk.look(job.t_begin + 2);
+    Look l2 = walk.look(job.t_begin + 2);
     for (int t = job.t_begin; t < job.t_end; ++t) {
       __syncthreads();  // every wave has written this tile, and has read the one before
       const Raw now = raw;
       if (t + 2 < job.t_end) raw = load(t + 2, l2);
       const Look l3 = walk.look(t + 3);
-      tile(t, (t - job.t_begin) & 1, now, lds, lds);
+      tile(t, (t - job.t_begin) & 1, is_page(a.map, l0.page) ? l0.pos : kHidden, now, lds, lds);
       l0 = l1;
       l1 = l2;
       l2 = l3;
@@ -809,6 +857,103 @@ __global__ __launch_bounds__(64 * KW) void fp4_few(PagedAttendArgs a) {
   few_body<T, D, KW, DV, NR>(a, job, lds);
 }
 
+// Joins the splits of a row: D / 4 lanes for four values each, GS of them a split apart, which take every GS-th split, NB at
+// a time, and are added up through LDS. With few rows many lanes a row: the loads of all splits are on their way at once (32
+// splits of 32 rows @J1@ us with 8 lanes, @J2@ with one).
+template <typename T, int D, int GS, int NB>
+__global__ __launch_bounds__(kPagedThreads) void fp4_join(PagedAttendArgs a) {
+  constexpr int kLanes = D / 4, kRows = kPagedThreads / (kLanes * GS);
+  __shared__ f32x4 part_x[GS > 1 ? kPagedThreads : 1];
+  __shared__ f32x4 part_s[GS > 1 ? kRows * GS : 1];
+  __shared__ int best[kRows];  // of the tokens that the workgroup has rows of
+  const long long rows = (long long)a.total * a.Hq, first = (long long)blockIdx.x * kRows;
+  const int tid = threadIdx.x, lane = tid % kLanes, g = tid / kLanes % GS, in = tid / (kLanes * GS);
+  if (tid < kRows) best[tid] = -1;
+  const long long row = min(first + in, rows - 1);
+  const int r = (int)(row / a.Hq);
+  f32x4 st[NB], y[NB];
+  auto load = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const long long at = min(s0 + GS * i, a.ns - 1) * rows + row;
+      st[i] = *(const f32x4*)(a.pml + at * 4);
+      y[i] = *(const f32x4*)(a.po + at * D + 4 * lane);
+    }
+  };
+  load(g);
+  // the sequences of the workgroup's first row, and from there on those that end before this row
+  int b = seq_of_row(a.q_start, a.map.B, (int)(first / a.Hq));
+  while (b < a.map.B && a.q_start[b + 1] <= r) ++b;
+  const bool some = b < a.map.B;
+  const Chunk c = some ? chunk_of(a.q_start, b, a.total) : Chunk{0, 0};
+  const int base = some ? a.base[b] : -1;
+  float M = -INFINITY, L = 0.f, SF = 0.f;
+  f32x4 x = {};
+  auto add = [&](const f32x4& s, const f32x4& v) __attribute__((always_inline)) {  // s: m, l, suffix sum of a share v
+    const float top = fmaxf(M, s[0]), ms = top == -INFINITY ? 0.f : top;
+    const float f0 = __builtin_amdgcn_exp2f(M - ms), f = __builtin_amdgcn_exp2f(s[0] - ms);
+    L = f0 * L + f * s[1];
+    SF = f0 * SF + f * s[2];
+    x = f0 * x + f * v;
+    M = top;
+  };
+  for (int s0 = g; s0 < a.ns; s0 += GS * NB) {
+    if (s0 > g) load(s0);
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+      if (s0 + GS * i < a.ns) add(st[i], y[i]);
+  }
+  if constexpr (GS > 1) {
+    part_x[tid] = x;
+    if (lane == 0) part_s[in * GS + g] = f32x4{M, L, SF, 0.f};
+    __syncthreads();
+    if (g == 0) {
+#pragma unroll
+      for (int i = 1; i < GS; ++i) add(part_s[in * GS + i], part_x[tid + i * kLanes]);
+    }
+  }
+  const bool live = g == 0 && first + in < rows && r >= c.first && r < c.first + c.n && c.n <= a.max_chunk && base >= 0 &&
+                    base <= a.map.cap - c.n;
+  const float inv = 1.f / L;
+  const float mass = L == 0.f ? 0.f : SF * inv;
+  if (a.conf != nullptr) {  // one atomic a workgroup and token
+    const int at = r - (int)(first / a.Hq);  // below kRows: a token has a row at least
+    const bool newest = live && r == c.first + c.n - 1;
+    __syncthreads();
+    if (lane == 0 && newest) atomicMax(best + at, conf_bits(mass));
+    __syncthreads();
+    const bool begins = row == first || row % a.Hq == 0;  // the token's first row here
+    if (lane == 0 && newest && begins) atomicMax((int*)a.conf + b, best[at]);
+  }
+  if (!live) return;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) x[e] = L == 0.f ? 0.f : x[e] * inv;
+  T* dst = (T*)a.out + row * D + 4 * lane;
+  if constexpr (sizeof(T) == 4)
+    *(f32x4*)dst = x;
+  else
+    *(u32x2_t*)dst = u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+  if (lane == 0) {
+    a.lse[row] = L == 0.f ? -INFINITY : kLn2 * (M + __builtin_amdgcn_logf(L));
+    if (a.suffix != nullptr) a.suffix[row] = mass;
+  }
+}
+
+template <typename T, int D, int GS, int NB>
+static void launch_join_as(const PagedAttendArgs& a, hipStream_t st) {
+  constexpr long kRows = kPagedThreads / (D / 4 * GS);
+  const long rows = (long)a.total * a.Hq;
+  hipLaunchKernelGGL((fp4_join<T, D, GS, NB>), dim3((unsigned)((rows + kRows - 1) / kRows)), dim3(kPagedThreads), 0, st, a);
+}
+template <typename T, int D>
+static void launch_join(const PagedAttendArgs& a, hipStream_t st) {
+  if (a.ns <= 2) launch_join_as<T, D, 1, 2>(a, st);
+  else if (a.ns <= 4) launch_join_as<T, D, 1, 4>(a, st);
+  else if (a.ns <= 16) launch_join_as<T, D, 4, 4>(a, st);
+  else if (a.ns <= 32) launch_join_as<T, D, 8, 4>(a, st);
+  else launch_join_as<T, D, 8, 8>(a, st);
+}
+
 // ------------------------------------------------------------------------------------------
 // Plan
 // ------------------------------------------------------------------------------------------
@@ -816,27 +961,59 @@ struct Fp4Plan {
   long many_tiles;  // upper bound over the chunks that `total` rows can be
   int ns;           // splits of a row's slots
   int halves;       // workgroups that share a row's output values (fp4_few)
-  bool few;         // fp4_few
+  int waves;        // of a workgroup of fp4_few: 8, or 16; 0: fp4_attend
 };
 
-constexpr long kFewTarget = 256, kManyTarget = 512;
-constexpr long kHalvesReach = 2560, kHalvesPairs = 64;
-constexpr long kMinSlots = 256, kSplitRows4 = 32;
-constexpr long kMaxSlots = 32768;  // of a split, whatever the number of workgroups
+// Decode steps (us in a graph, 28 / 4 or 32 / 8 heads of 128, bfloat16, at capacities of 1024 / 2048 / 4096 / 16384 slots,
+// 640 to 1024, ... live). A CU holds one workgroup of 16 waves or two of 8 (of at most 16 rows).
+//   up to 64 pairs of a sequence and a KV head: one workgroup a CU by splits. 32 pairs in 1 / 4 / 8 splits 9.8 15.9 26.0 85.1 /
+//     9.2 11.0 13.3 29.1 / 9.6 10.4 12.8 20.7; 8 pairs and 4096 slots in 4 / 8 / 16 / 32 splits 12.2 11.1 9.8 9.7.
+//   up to 128: one launch without a split is ahead on short caches: at 128 values two halves of 16 waves, up to 2560 slots
+//     (128 pairs, halves / four splits 10.7 14.5 21.5 69.3 / 12.8 15.8 20.6 56.6), at 64 values 16 waves, up to 1536 (9.6 13.2 19.8
+//     58.5 / 10.8 12.9 16.1 36.5). Behind that two workgroups a CU by splits.
+//   up to 256: 16 waves, no split (192 pairs 12.0 16.5 25.3 79.8, 8 waves 12.5 18.2 29.8 95.7, in two splits 15.4 19.8 28.0 83.6).
+//   more: 8 waves, no split (512 pairs of up to 8192 slots 97; with 16 waves 99).
+// float32 at 128 values has registers for 8 waves alone, one workgroup a CU, and halves win up to 1024 slots (128 pairs, halves /
+// two splits 14.5 20.2 31.6 / 15.0 18.8 25.9); so have steps of 17 to 32 rows (128 pairs of 28 rows 14.7 33.9 / 15.9 27.6 at
+// 1024 / 4096).
+constexpr long kFewCUs = 256, kFewUnsplit = 64, kFewWhole = 128;
+constexpr long kFewSlots = 256;  // of a split at least: the launch that joins takes 1.3 us more than it saves a cache of 256 slots
+// Workgroups that a launch with long chunks aims for by splitting slots. The mixed step (4 sequences of 128 tokens, 12 that decode,
+// a window of 2048) unsplit / in 2 / 3 / 4 splits: 63.8 / 46.1 / 49.4 / 52.9 us; 256 tokens behind 16128 slots in 4 / 6 / 8 / 16: 106 / 109 /
+// 91 / 103; 64 behind 8128 in 8 / 16 / 32: 33.9 / 27.0 / 30.9; 2048 behind 6144 unsplit / in 2: 249 / 259.
+constexpr long kManyTarget = 512;
+// Slots of a split there: 256, and one for every 32 query rows of the launch, whose partials are written and read.
+constexpr long kManySlots = 256, kRowsPerSlot = 32;
+// Slots of a split at most, whatever the number of workgroups: the capacity is all that the host knows, and one long sequence
+// among many short ones shall not hold up the launch.
+constexpr long kMaxSlots = 32768;
 constexpr long kMaxSplits = 64;
-constexpr long kMaxJoined = (1l << 27) - 8;  // rows that the joining launch has a grid for
+// Rows that a launch joins at most: its 256 threads a workgroup of one row at least must stay below the 2^32 of a grid.
+constexpr long kMaxJoined = (1l << 24) - 1;
 
-static Fp4Plan fp4_plan(const lg_paged_layer& l, const lg_page_map& m, lg_dtype, long total, long max_chunk, long reach) {
+// reach: slots that a token may see, by the capacity and the window.
+static Fp4Plan fp4_plan(const lg_paged_layer& l, const lg_page_map& m, lg_dtype dtype, long total, long max_chunk, long reach) {
   const long G = l.n_q_heads / l.n_kv_heads;
-  Fp4Plan p;
-  p.many_tiles = 0;
-  p.halves = 1;
-  p.few = max_chunk * G <= kWaveRows;
-  long ns, slots = kMinSlots;
-  if (p.few) {
+  const bool wide = l.head_dim == 128;
+  Fp4Plan p = {0, 1, 1, 0};
+  long ns = 1, slots = kFewSlots;
+  if (max_chunk * G <= kWaveRows) {
+    const bool two = max_chunk * G <= 16 && !(dtype == LG_F32 && wide);  // two workgroups of 8 waves fit a CU, or one of 16
     const long units = (long)m.batch * l.n_kv_heads;
-    ns = kFewTarget / units;
-    if (ns > 2 && units >= kHalvesPairs && reach <= kHalvesReach && l.head_dim == 128) ns = 2;
+    const long whole = !wide ? 1536 : dtype == LG_F32 ? 1024 : 2560;
+    p.waves = 8;
+    if (units <= kFewUnsplit) {
+      ns = kFewCUs / units;
+    } else if (units <= kFewWhole) {
+      if (reach > whole) {
+        ns = (two ? 2 : 1) * kFewCUs / units;
+      } else {
+        p.halves = wide ? 2 : 1;
+        p.waves = two ? 16 : 8;
+      }
+    } else if (units <= kFewCUs) {
+      p.waves = two ? 16 : 8;
+    }
   } else {
     if (total * G > kWaveRows) {
       // a sequence of n rows has at most n / 128 + 1 tiles, and more than 32 rows
@@ -845,15 +1022,10 @@ static Fp4Plan fp4_plan(const lg_paged_layer& l, const lg_page_map& m, lg_dtype,
     }
     const long units = (p.many_tiles + m.batch) * l.n_kv_heads;
     ns = (kManyTarget + units - 1) / units;
-    slots += total * l.n_q_heads / kSplitRows4;
+    slots = kManySlots + total * l.n_q_heads / kRowsPerSlot;
   }
   ns = std::min({ns, (reach + slots - 1) / slots, kMaxSplits});
-  const long least = std::min(reach / kMaxSlots, kMaxSplits);
-  if (p.few && ns == 2 && least < 2 && l.head_dim == 128) {
-    ns = 1;
-    p.halves = 2;
-  }
-  p.ns = (int)std::max({ns, least, 1l});
+  p.ns = (int)std::max({ns, std::min(reach / kMaxSlots, kMaxSplits), 1l});
   if (total * l.n_q_heads > kMaxJoined) p.ns = 1;
   return p;
 }
@@ -905,14 +1077,16 @@ static void launch_few(const PagedAttendArgs& a, const Fp4Plan& p, dim3 grid, hi
 
 template <typename T, int D>
 static void launch_typed(const PagedAttendArgs& a, const Fp4Plan& p, dim3 grid, hipStream_t st) {
-  constexpr int KW = 8;
-  if (!p.few)
+  if (p.waves == 0) {
     hipLaunchKernelGGL((fp4_attend<T, D>), grid, dim3(kPagedThreads), 0, st, a);
-  else if ((long)a.max_chunk * a.G <= 16)
-    launch_few<T, D, KW, 1>(a, p, grid, st);
-  else
-    launch_few<T, D, KW, 2>(a, p, grid, st);
-  if (p.ns > 1) launch_paged_join(a, sizeof(T) == 2, D, st);
+  } else if ((long)a.max_chunk * a.G > 16) {
+    launch_few<T, D, 8, 2>(a, p, grid, st);
+  } else if (p.waves == 8) {
+    launch_few<T, D, 8, 1>(a, p, grid, st);
+  } else if constexpr (sizeof(T) == 2 || D == 64) {
+    launch_few<T, D, 16, 1>(a, p, grid, st);
+  }
+  if (p.ns > 1) launch_join<T, D>(a, st);
 }
 
 hipError_t launch_fp4_attend(const lg_paged_layer& l, const lg_page_map& m, lg_dtype dtype, const void* q, void* out,

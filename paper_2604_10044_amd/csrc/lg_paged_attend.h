@@ -1,5 +1,5 @@
 // lg_paged_attend.h -- what the attention kernels over pages share (lg_paged_attend.hip, lg_fp4_attend.hip): their
-// arguments, the rows and slots of a workgroup, the statistics of a row, the launch that joins splits.
+// arguments, the rows and slots of a workgroup, the statistics of a row.
 #pragma once
 
 #include <algorithm>
@@ -204,8 +204,5 @@ inline long whole_reach(const lg_page_map& m) { return (long)m.max_pages * m.pag
 inline long window_reach(const lg_page_map& m, long max_chunk, long window, long n_sink) {
   return window > 0 ? std::min(whole_reach(m), window + n_sink + max_chunk) : whole_reach(m);
 }
-
-// The launch behind one whose slots were split (T, D: as the layer's queries).
-void launch_paged_join(const PagedAttendArgs& a, bool bf16, int D, hipStream_t st);
 
 }  // namespace lg

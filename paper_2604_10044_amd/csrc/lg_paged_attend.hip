@@ -909,23 +909,6 @@ __global__ __launch_bounds__(kPagedThreads) void paged_join(PagedAttendArgs a) {
   }
 }
 
-template <typename T, int D>
-static void launch_join_typed(const PagedAttendArgs& a, hipStream_t st) {
-  const long rows = (long)a.total * a.Hq;
-  hipLaunchKernelGGL((paged_join<T, D>), dim3((unsigned)((rows + join_rows<D>() - 1) / join_rows<D>())), dim3(kPagedThreads), 0,
-                     st, a);
-}
-
-void launch_paged_join(const PagedAttendArgs& a, bool bf16, int D, hipStream_t st) {
-  if (bf16) {
-    if (D == 128) launch_join_typed<__bf16, 128>(a, st);
-    else launch_join_typed<__bf16, 64>(a, st);
-  } else {
-    if (D == 128) launch_join_typed<float, 128>(a, st);
-    else launch_join_typed<float, 64>(a, st);
-  }
-}
-
 // ------------------------------------------------------------------------------------------
 // Plan and launch
 // ------------------------------------------------------------------------------------------
@@ -1044,7 +1027,10 @@ static void launch_typed(const PagedAttendArgs& a, const PagedPlan& p, dim3 grid
   } else {
     launch_few<T, D, KW, 32>(a, p, grid, st);
   }
-  if (p.ns > 1) launch_join_typed<T, D>(a, st);
+  const long rows = (long)a.total * a.Hq;
+  if (p.ns > 1)
+    hipLaunchKernelGGL((paged_join<T, D>), dim3((unsigned)((rows + join_rows<D>() - 1) / join_rows<D>())), dim3(kPagedThreads), 0,
+                       st, a);
 }
 
 hipError_t launch_paged_attend(const lg_paged_layer& l, const lg_page_map& m, const void* q, void* out,
