@@ -22,7 +22,7 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 template <typename T> constexpr int q_terms() { return sizeof(T) == 4 ? 3 : 1; }
 template <typename T, bool FEW> constexpr int p_terms() { return sizeof(T) == 4 ? 3 : FEW ? 2 : 1; }
 
-// Two weights as N bfloat16 terms, each what the ones before leave, to nearest: with two within 2^-17, with three exact.
+// Two weights as N bfloat16 terms, each what the ones before leave, to nearest: with two within 2^-16, with three exact.
 template <int N>
 __device__ __forceinline__ void weight_terms(float x, float y, uint32_t (&t)[N]) {
 #pragma unroll
@@ -559,6 +559,19 @@ struct Many {
   static __device__ __forceinline__ int turn_v(int row) { return 5 * (D == 128 ? row & 3 : (row >> 1) & 1); }
 };
 
+// Order for the scheduler: the 8 reads of LDS and 8 matrix instructions of a tile's scores at head_dim 64, the reads 4 ahead
+// (4096 tokens behind 4096, 32 / 8 heads: 298 us left to itself, 280 so; at head_dim 128 431 and 435, in float32 1081 and
+// 1123).
+__device__ __forceinline__ void schedule_scores() {
+  __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);  // reads of LDS
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);  // matrix instructions
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);
+}
+
 template <typename T, int D>
 __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, char* lds) {
   using C = Many<D>;
@@ -731,6 +744,7 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
     f32x16 S, S1;
     scores(from, here, S);
     scores(from, here + kBlock, S1);
+    if constexpr (D == 64 && QT == 1) schedule_scores();
     if (masked) {
       mask(S, s0, 0);
       mask(S1, s0, 1);
