@@ -73,7 +73,8 @@ typedef struct {
 } lg_page_map;
 
 /* One layer's pages: k, v [n_pages][n_kv_heads][page_size][head_dim] of dtype. Supported sizes and
- * types as in lg_layer_cache; n_pages and page_size as in the map (LG_ERR_SHAPE). */
+ * types as in lg_layer_cache; n_pages and page_size as in the map (LG_ERR_SHAPE). lg_page_reserve and lg_page_compact
+ * also take layers of LG_FP4 (lg_fp4.h). */
 typedef struct {
   int32_t n_pages, page_size, n_q_heads, n_kv_heads, head_dim;
   lg_dtype dtype;
