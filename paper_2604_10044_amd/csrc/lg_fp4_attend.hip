@@ -139,16 +139,12 @@ struct Walk {
   }
 };
 
-// Where row `row` of a page and its exponents lie in K or V (a page that is none: page 0). Blocks have at least 544
-// bytes, so their numbers stay below 2^32 in any memory.
-struct Block {
-  size_t rows, exps;
-};
+// Where a page of the workgroup's KV head lies in K or V (a page that is none: page 0). Blocks have at least 544 bytes, so
+// their numbers stay below 2^32 in any memory.
 template <int D>
-__device__ __forceinline__ Block block_at(const PagedAttendArgs& a, const Job& job, int page, int row) {
+__device__ __forceinline__ size_t block_at(const PagedAttendArgs& a, const Job& job, int page) {
   const unsigned n = (unsigned)(is_page(a.map, page) ? page : 0) * (unsigned)a.Hkv + (unsigned)job.h;
-  const size_t at = (size_t)n * fp4_block(D, a.map.shift);
-  return {at + (long)row * (D / 2), at + ((size_t)(D / 2) << a.map.shift) + (long)row * (D / 32)};
+  return (size_t)n * (unsigned)fp4_block(D, a.map.shift);
 }
 
 // What a row of the wave sees: slots up to its own, at positions above win or below n_sink; it counts those above
@@ -169,19 +165,21 @@ __device__ __forceinline__ bool sees(const PagedAttendArgs& a, const Sight& s, i
 }
 
 // How a tile of NK slots from s0 on, with the lane's slot at position tp, is to be compared: whether some row may not
-// see a slot (lo: the first row's own slot, win_hi: the last row's window), and what it has of the suffix.
+// see a slot (lo, hi: the first and the last row), and what it has of the suffix.
 enum { kNone, kAll, kSome };
+struct Compare {
+  bool masked;
+  int suffix;
+};
 template <int NK>
-__device__ __forceinline__ bool is_masked(const PagedAttendArgs& a, int tp, int s0, int lo, int win_hi) {
+__device__ __forceinline__ Compare compare_of(const PagedAttendArgs& a, int tp, int s0, const Sight& lo, const Sight& hi) {
   const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
-  return __ballot(tp == kHidden) != 0 || s0 + NK - 1 > lo || (a.window > 0 && p_first <= win_hi && p_last >= a.n_sink);
-}
-template <int NK>
-__device__ __forceinline__ int suffix_of(const PagedAttendArgs& a, int tp, int suf_lo, int suf_hi) {
-  if (a.suffix == nullptr && a.conf == nullptr) return kNone;
-  const int p_first = __builtin_amdgcn_readlane(tp, 0), p_last = __builtin_amdgcn_readlane(tp, NK - 1);
+  Compare c;
+  c.masked = __ballot(tp == kHidden) != 0 || s0 + NK - 1 > lo.slot || (a.window > 0 && p_first <= hi.win && p_last >= a.n_sink);
   // kHidden in front says nothing about the slots behind it
-  return p_last <= suf_lo ? kNone : p_first > suf_hi && p_first != kHidden ? kAll : kSome;
+  c.suffix = p_last <= lo.suf ? kNone : p_first > hi.suf && p_first != kHidden ? kAll : kSome;
+  if (a.suffix == nullptr && a.conf == nullptr) c.suffix = kNone;
+  return c;
 }
 
 // LDS of a wave beside its tiles: 64 bounds (a row sees slot j if bound_j > win and the slot is none behind its own), 64
@@ -273,21 +271,24 @@ __device__ __forceinline__ void few_body(const PagedAttendArgs& a, Job job, char
   auto load = [&](int t, const Pages& p) __attribute__((always_inline)) {
     Raw raw;
     const int s0 = walk.slot_of(t), most = last_slot - s0;
-    const Block first = block_at<D>(a, job, p.first, s0 & (ps - 1));
-    // as if the second page began 16 rows earlier
-    const Block second = short_pages && most >= 16 ? block_at<D>(a, job, p.second, -16) : first;
+    // Rows from 16 on lie in the second page where a page is 16 slots.
+    const bool two = short_pages && most >= 16;
+    const size_t first = block_at<D>(a, job, p.first), second = two ? block_at<D>(a, job, p.second) : first;
+    const int row0 = s0 & (ps - 1), row1 = two ? -16 : row0;
 #pragma unroll
     for (int j = 0; j < NJ; ++j) {
-      const unsigned row = min(16 * j + col, most);
-      raw.k[j] = at32((const KRow*)((const char*)a.k + (j == 0 ? first : second).rows), row * RB + part * (RB / 4));
-      raw.ke[j] = at32((const uint8_t*)a.k + (j == 0 ? first : second).exps, row * EB + (D == 128 ? part : part >> 1));
+      const unsigned row = min(16 * j + col, most) + (j == 0 ? row0 : row1);
+      const char* at = (const char*)a.k + (j == 0 ? first : second);
+      raw.k[j] = at32((const KRow*)at, row * RB + part * (RB / 4));
+      raw.ke[j] = at32((const uint8_t*)at, ps * RB + row * EB + (D == 128 ? part : part >> 1));
     }
 #pragma unroll
     for (int u = 0; u < VU; ++u) {
-      const unsigned row = min(lane / VP + u * (64 / VP), most);
       const bool later = VP == 4 ? u == 1 : lane >= 32;
-      raw.v[u] = at32((const u32x4_t*)((const char*)a.v + job.d0 / 2 + (later ? second : first).rows), row * RB + lane % VP * 16);
-      raw.ve[u] = at32((const uint8_t*)a.v + job.d0 / 32 + (later ? second : first).exps, row * EB + lane % VP);
+      const unsigned row = min(lane / VP + u * (64 / VP), most) + (later ? row1 : row0);
+      const char* at = (const char*)a.v + (later ? second : first);
+      raw.v[u] = at32((const u32x4_t*)at, row * RB + job.d0 / 2 + lane % VP * 16);
+      raw.ve[u] = at32((const uint8_t*)at, ps * RB + row * EB + job.d0 / 32 + lane % VP);
     }
     raw.pos = walk.pos_of_lane(s0);
     raw.pages = p;
@@ -375,10 +376,9 @@ __device__ __forceinline__ void few_body(const PagedAttendArgs& a, Job job, char
     }
   };
   auto finish = [&]() __attribute__((always_inline)) {
-    const bool masked = is_masked<NK>(a, tp, s0, lo.slot, hi.win);
-    const int how = suffix_of<NK>(a, tp, lo.suf, hi.suf);
-    if (masked || how == kSome) note(a, notes, tp);
-    if (masked) {
+    const Compare is = compare_of<NK>(a, tp, s0, lo, hi);
+    if (is.masked || is.suffix == kSome) note(a, notes, tp);
+    if (is.masked) {
 #pragma unroll
       for (int j = 0; j < NJ; ++j) {
         const i32x4 bound = *(const i32x4*)(notes + 16 * j + 4 * part);
@@ -419,8 +419,8 @@ __device__ __forceinline__ void few_body(const PagedAttendArgs& a, Job job, char
         for (int i = 0; i < 2; ++i) weight_terms<PT>(S[n][j][2 * i], S[n][j][2 * i + 1], P[n][j / 2][2 * (j & 1) + i]);
       }
       l[n] += sum;
-      sfx[n] += how == kAll ? sum : 0.f;
-      if (how == kSome) {
+      sfx[n] += is.suffix == kAll ? sum : 0.f;
+      if (is.suffix == kSome) {
 #pragma unroll
         for (int j = 0; j < NJ; ++j) {
           const i32x4 p = *(const i32x4*)(notes + 64 + 16 * j + 4 * part);
@@ -598,9 +598,11 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
   const Sight sight = sight_of(a, job.base + tok, pos[job.base + tok], a.suffix_w != nullptr ? a.suffix_w[job.b] : 0);
   skip_hidden<NK>(a, job, pos);
   // bounds over the wave's rows (tokens ascend with the row, positions with the token)
-  const int slot_lo = __builtin_amdgcn_readlane(sight.slot, 0), slot_hi = __builtin_amdgcn_readlane(sight.slot, 31);
-  const int win_hi = __builtin_amdgcn_readlane(sight.win, 31);
-  const int suf_lo = __builtin_amdgcn_readlane(sight.suf, 0), suf_hi = __builtin_amdgcn_readlane(sight.suf, 31);
+  const auto row_of = [&](int lane_of) __attribute__((always_inline)) {
+    return Sight{__builtin_amdgcn_readlane(sight.slot, lane_of), __builtin_amdgcn_readlane(sight.win, lane_of),
+                 __builtin_amdgcn_readlane(sight.suf, lane_of)};
+  };
+  const Sight lo = row_of(0), hi = row_of(31);
 
   f32x16 O[ND];
 #pragma unroll
@@ -617,11 +619,11 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
   const int in = lane >> 2, quarter = lane & 3;
   auto load = [&](int t, const Look& lk) __attribute__((always_inline)) {
     const int s0 = min(walk.slot_of(t) + 16 * wave, last_slot & ~15);  // rows behind last_slot repeat it
-    const Block at = block_at<D>(a, job, __builtin_amdgcn_readlane(lk.page, 16 * wave), s0 & (ps - 1));
-    const unsigned row = min(in, last_slot - s0);
-    const unsigned off = row * RB + quarter * (RB / 4), ea = row * EB + (D == 128 ? quarter : quarter >> 1);
-    return Raw{at32((const Quarter*)((const char*)a.k + at.rows), off), at32((const Quarter*)((const char*)a.v + at.rows), off),
-               at32((const uint8_t*)a.k + at.exps, ea), at32((const uint8_t*)a.v + at.exps, ea)};
+    const size_t at = block_at<D>(a, job, __builtin_amdgcn_readlane(lk.page, 16 * wave));
+    const unsigned row = (s0 & (ps - 1)) + min(in, last_slot - s0);
+    const unsigned off = row * RB + quarter * (RB / 4), ea = ps * RB + row * EB + (D == 128 ? quarter : quarter >> 1);
+    const char *k = (const char*)a.k + at, *v = (const char*)a.v + at;
+    return Raw{at32((const Quarter*)k, off), at32((const Quarter*)v, off), at32((const uint8_t*)k, ea), at32((const uint8_t*)v, ea)};
   };
   const int w_row = 16 * wave + in, w_at = w_row * RBV;
   auto store = [&](const Raw& raw, int buffer, char* __restrict__ to) __attribute__((always_inline)) {
@@ -719,15 +721,14 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
   // Tile t from its buffer, while the next one's rows go to the other buffer. The two are pointers that do not alias: the
   // reads need not wait for the writes.
   auto tile = [&](int t, int buffer, int tp, const Raw& raw, const char* __restrict__ from, char* __restrict__ to) __attribute__((always_inline)) {
+    const uint32_t flags = *(const uint32_t*)(from + C::kFlags + 256 * buffer + 4 * lane);
     if (t + 1 < job.t_end) store(raw, buffer ^ 1, to);
     const int s0 = walk.slot_of(t);
-    if (idle || s0 > slot_hi) return;
+    if (idle || s0 > hi.slot) return;
     const int here = buffer * C::kBuffer;
     constexpr int kBlock = 32 * RBV;
-    const bool masked = is_masked<NK>(a, tp, s0, slot_lo, win_hi);
-    const int how = suffix_of<NK>(a, tp, suf_lo, suf_hi);
-    if (masked || how == kSome) note(a, notes, tp);
-    const uint32_t flags = *(const uint32_t*)(from + C::kFlags + 256 * buffer + 4 * lane);
+    const Compare is = compare_of<NK>(a, tp, s0, lo, hi);
+    if (is.masked || is.suffix == kSome) note(a, notes, tp);
     unsigned long long odd = __ballot(flags != 0);
     for (; odd != 0; odd &= odd - 1) {  // values that stand for NaN: in their 32 values of the rows that see the slot
       const int key = __builtin_ctzll(odd);
@@ -745,7 +746,7 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
     scores(from, here, S);
     scores(from, here + kBlock, S1);
     if constexpr (D == 64 && QT == 1) schedule_scores();
-    if (masked) {
+    if (is.masked) {
       mask(S, s0, 0);
       mask(S1, s0, 1);
     }
@@ -755,8 +756,8 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
     sum += weights(S1);
     product(from, here + C::kTile + kBlock, S1);
     l += sum;
-    sfx += how == kAll ? sum : 0.f;
-    if (how == kSome) {
+    sfx += is.suffix == kAll ? sum : 0.f;
+    if (is.suffix == kSome) {
       add_suffix(S, 0);
       add_suffix(S1, 1);
     }
