@@ -313,6 +313,75 @@ def test_unpack(dtype, D, hkv, ps):
             np.testing.assert_array_equal(o.double().cpu().numpy(), want)
 
 
+@pytest.mark.parametrize("total", [2047, 2048, 5000, 9000, 30000])
+def test_unpack_of_many_slots(total):
+    """Batches whose workgroups read 1 to 16 slots each: sequences that begin and end inside one, empty ones, rows before the
+    first and behind the last sequence, missing pages and refused sequences."""
+    from paper_2604_10044_amd import lg
+    r = np.random.RandomState(total)
+    ps, hkv, D = 16, 2, 64
+    lens = []
+    while sum(lens) < total - 5:
+        lens.append(int(min(r.choice([0, 1, 2, 5, 17, 100, 700]), total - 5 - sum(lens))))
+    B, P = len(lens), max(1, -(-max(lens) // ps))
+    pages = [-(-n // ps) for n in lens]
+    table, at = np.full((B, P), -1), 0
+    order = r.permutation(sum(pages) + 1)
+    for b in range(B):
+        table[b, :pages[b]] = order[at:at + pages[b]]
+        at += pages[b]
+    holes = (table >= 0) & (r.rand(B, P) < 0.02)
+    table[holes] = r.choice([-1, 10 ** 9], int(holes.sum()))
+    k, v = (r.randint(0, 256, (len(order), hkv, lg.fp4_page_bytes(ps, D))).astype(np.uint8) for _ in range(2))
+    k[..., ps * D // 2:], v[..., ps * D // 2:] = 120, 130
+    i32 = lambda x: torch.as_tensor(np.asarray(x, np.int32), device="cuda")  # noqa: E731
+    layer = lg.paged_layer_fp4(torch.as_tensor(k, device="cuda"), torch.as_tensor(v, device="cuda"), hkv, ps, D)
+    m = lg.page_map(i32(table), i32(np.zeros((B, P * ps))), i32(lens), i32(np.ones(len(order))), ps)
+    start, base = 3 + np.concatenate([[0], np.cumsum(lens)]), np.where(r.rand(B) < 0.05, -1, 0)
+    ko, vo = (torch.full((total, hkv, D), 9.0, device="cuda", dtype=F32) for _ in range(2))
+    lg.lg_page_unpack_fp4(layer, m, ko, vo, i32(start), i32(base))
+    torch.cuda.synchronize()
+    seq = np.repeat(np.arange(B), lens)
+    slot = np.concatenate([np.arange(n) for n in lens])
+    page = table[seq, slot // ps]
+    live = (base[seq] >= 0) & (page >= 0) & (page < len(order))
+    for x, o in ((k, ko), (v, vo)):
+        want = np.full((total, hkv, D), 9.0)
+        val = fp4.values(*fp4.unpack(x, ps, D))
+        want[3 + np.flatnonzero(live)] = val[page[live], :, slot[live] % ps]
+        np.testing.assert_array_equal(o.double().cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("bits", [4, 16])
+def test_many_sequences(bits):
+    """More sequences than a wave looks at together, some without tokens."""
+    n = [(b * 7) % 4 for b in range(150)]
+    s = Step(BF, bits, 64, 4, 2, 16, [(b * 5) % 30 for b in range(150)], n, axes=3, seed=11)
+    was = s.state()
+    f = _freq(64)
+    s.call(f, 64, axis=np.arange(32) % 3)
+    s.check(f, 64, False, 1.0, was)
+
+
+def test_rows_before_the_first_sequence():
+    """q_start need not begin at 0: rows before it are no sequence's."""
+    s = Step(BF, 4, 64, 4, 2, 16, [4, 9], [7, 3], seed=12, extra=6)
+    was = s.state()
+    s.q_start.add_(5)
+    f = _freq(64)
+    s.call(f, 64)
+    got = s.state()
+    assert (got[2][:5] == 3).all() and (got[2][15:] == 3).all() and (got[2][5:15] != 3).any(-1).all()
+    # the same as with the rows in front
+    t = Step(BF, 4, 64, 4, 2, 16, [4, 9], [7, 3], seed=12, extra=6)
+    t.qkv[:10] = s.qkv[5:15]
+    t.call(f, 64)
+    for x, y in zip(got[:2], t.state()[:2]):
+        np.testing.assert_array_equal(x, y)
+    np.testing.assert_array_equal(got[2][5:15], t.state()[2][:10])
+    del was
+
+
 def test_append_then_unpack_on_another_stream_and_in_a_graph():
     """An append and a read back, captured and replayed with other rows and places, against eager calls."""
     from paper_2604_10044_amd import lg

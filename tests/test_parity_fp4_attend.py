@@ -124,6 +124,10 @@ def test_long(dtype, D, hq, hkv, ps, have, n, window, sinks):
 @pytest.mark.parametrize("dtype,D,hq,hkv,batch", [
     (BF, 128, 4, 4, 32), (BF, 128, 14, 2, 45), (BF, 128, 8, 1, 70), (F32, 128, 4, 2, 50), (BF, 64, 16, 4, 32), (BF, 128, 8, 8, 40),
     (F32, 64, 16, 1, 130),
+    (BF, 128, 8, 4, 50),      # 200 pairs: 16 waves a workgroup
+    (BF, 64, 12, 4, 40),
+    (F32, 128, 8, 4, 50),
+    (BF, 128, 40, 40, 3),     # one query head a KV head
 ])
 def test_decode_batches(dtype, D, hq, hkv, batch):
     """A token a sequence at batch sizes that take each launch of the decode step."""
@@ -145,6 +149,48 @@ def test_few_rows(dtype, D, hq, hkv, have, n):
     a = Attend4(dtype, D, hq, hkv, 16, have, n, seed=sum(n) + D)
     a.call()
     a.check(tokens=np.array([0, 1, 3, 4, -1]))
+
+
+@pytest.mark.parametrize("dtype,D,hq,hkv,have,n", [
+    (BF, 128, 8, 2, [2900] + [60] * 39, [1] * 40),   # 80 pairs of long capacity: splits, two workgroups a CU
+    (BF, 128, 14, 2, [2900] + [60] * 39, [4] + [1] * 39),  # of 28 rows: one a CU
+    (BF, 64, 8, 2, [1900] + [60] * 39, [1] * 40),
+    (F32, 128, 8, 2, [1500] + [60] * 39, [1] * 40),
+    (F32, 64, 8, 2, [1900] + [60] * 39, [2] * 40),
+    (BF, 128, 8, 8, [9000], [1]),                    # 32 splits, and 64
+    (BF, 64, 4, 1, [17000], [2]),
+    (F32, 128, 4, 1, [17000], [1]),
+])
+def test_splits(dtype, D, hq, hkv, have, n):
+    a = Attend4(dtype, D, hq, hkv, 32, have, n, seed=sum(n) + D)
+    a.call()
+    a.check()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n", [1, 6, 50])
+def test_nan_in_one_of_several_splits(dtype, n):
+    """Keys and values that stand for NaN in a slot that one split of several has."""
+    for which in (0, 1):
+        a = Attend4(dtype, 128, 8, 2, 16, [3000, 70], [n, 1], seed=26, holes=False)
+        a.call()
+        want = a.results()
+        assert np.isfinite(want[0][:n + 1]).all()
+        p = int(a.table_h[0, 1234 // 16])
+        a.exponents(which)[p, 1, 1234 % 16, 3] = 255
+        a.call()
+        got = a.results()
+        rows, heads = slice(0, n), slice(4, 8)
+        if which == 0:
+            assert np.isnan(got[0][rows, heads]).all() and np.isnan(got[1][rows, heads]).all() and np.isnan(got[3][0])
+            for x, y in zip(got[:3], want[:3]):
+                x[rows, heads] = y[rows, heads]
+            got[3][0] = want[3][0]
+        else:
+            assert np.isnan(got[0][rows, heads, 96:]).all()
+            got[0][rows, heads, 96:] = want[0][rows, heads, 96:]
+        for x, y in zip(got, want):
+            np.testing.assert_array_equal(x, y)
 
 
 @pytest.mark.parametrize("dtype,D,hq,hkv,n", [(BF, 128, 8, 2, [1, 4, 8]), (BF, 64, 16, 1, [1, 2, 2]), (BF, 128, 4, 4, [16, 20, 32])])
