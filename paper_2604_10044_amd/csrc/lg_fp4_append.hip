@@ -5,6 +5,9 @@
 // two that has m <= 6 u, and c_i is x_i / u to the nearest of 0, 0.5, 1, 1.5, 2, 3, 4, 6 (the conversion instruction's
 // rounding: ties to the even code, a tie being the same as the definition's in every unit). A lane holds 8 values, so
 // a group is four lanes of a row of 16 and m two exchanges between neighbours.
+//
+// Memory bounds long chunks: two prompts of 8192 tokens of 32 / 8 heads of 128 in bfloat16 on three axes, 354 MB, 71 us, 5.0 TB/s (a
+// copy reaches 5.13). A decode step's append is a chain of dependent reads and one launch: 3.9 us for 32 sequences.
 #include "lg_fp4.h"
 #include "lg_rope.h"
 

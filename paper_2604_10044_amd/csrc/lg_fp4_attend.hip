@@ -7,6 +7,22 @@
 // and V become bfloat16 in registers, and both products are bfloat16 matrix instructions whose products are exact. float32
 // queries and weights enter as three bfloat16 terms each (8 + 8 + 8 bits, exact), three times the instructions, still
 // a fifth of what float32 ones would take.
+//
+// What bounds it, measured on MI355X (a copy reaches 5.13 TB/s, a bfloat16 matrix product of 8192^3 1122 TFLOP/s), in a
+// graph: 64 sequences of 8192 slots, 32 / 8 heads of 128, 471 MB, 97 us, 4.85 TB/s: the memory. A decode step of 32 sequences of 28 / 4
+// heads and 1280 to 2047 slots, 30 MB, 14.4 us: its chain and its instructions. The sequence is known after 0.9 us, the first
+// rows are asked for after 2.0, the first tile of 32 slots is done after 4.2, and each further one takes a wave 1.2 us beside
+// the others of its SIMD (230 vector and 16 matrix instructions, 100 scalar ones); the bytes alone would take 6. 4096 tokens of
+// 32 / 8 heads behind 4096, 412 GFLOP, 420 to 434 us, 950 to 980 TFLOP/s: matrix instructions, with the conversions and
+// exponentials beside them in part; in float32 1085 us, 380 TFLOP/s of exact products. Four sequences of 128 tokens with a window of
+// 2048 beside 12 that decode, 44 us: a workgroup's chain, 17 tiles of 2 us with one wave on a SIMD, and the launch that joins two splits.
+//
+// Tried and left (us, the decode step of 32 sequences / 64 sequences of 8192 slots unless said): tiles two to four ahead in
+// registers (16.7 to 17.6 against 15.8 / 103 to 109 against 97: the copies of their registers wait for all of them); the
+// exponents of a row in one load, spread by permutes (18.4 / 139); tiles of 64 slots (15.7 against 16.0 / 103 against 101); 4 waves
+// a workgroup (18.3 against 16.0). Chunks: the scores of both blocks of 32 keys side by side, or the next tile's conversion among
+// them (4096 tokens 510 to 640: registers); two teams of four waves a workgroup that share out the tiles (8 sequences of 128 tokens,
+// window 1024, 28.5 against 31.4, the mixed step 51 against 46: one barrier keeps the teams in step).
 #include "lg_fp4.h"
 #include "lg_paged_attend.h"
 
@@ -874,7 +890,7 @@ __global__ __launch_bounds__(64 * KW) void fp4_few(PagedAttendArgs a) {
 
 // Joins the splits of a row: D / 4 lanes for four values each, GS of them a split apart, which take every GS-th split, NB at
 // a time, and are added up through LDS. With few rows many lanes a row: the loads of all splits are on their way at once (32
-// splits of 32 rows @J1@ us with 8 lanes, @J2@ with one).
+// splits of 32 rows 4.0 us with 8 lanes, 6.6 with one; two splits of 16800 rows 6.7 with two at a time, 8.6 with eight).
 template <typename T, int D, int GS, int NB>
 __global__ __launch_bounds__(kPagedThreads) void fp4_join(PagedAttendArgs a) {
   constexpr int kLanes = D / 4, kRows = kPagedThreads / (kLanes * GS);

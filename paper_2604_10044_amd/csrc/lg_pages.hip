@@ -424,7 +424,8 @@ constexpr uint32_t kStays = 0xffffffffu;
 // page_size + row: below 2^32, since a slot has 128 bytes at least).
 // Memory bounds it: 3.0 GB in 534 us, 5.6 TB/s, where a copy of 1 GiB runs at 5.2.
 //
-// 4-bit rows (L = 4 or 2 lanes of 16 bytes, in place of 8): an item is the whole row with its exponents, a byte a lane.
+// 4-bit rows (L = 4 or 2 lanes of 16 bytes, in place of 8): an item is the whole row with its exponents, a byte a lane. The same
+// moves in 4 bits, 0.79 GB: 171 us, 4.6 TB/s; one sequence of 28 layers 11.8 us (35.4 in bfloat16).
 template <int L>
 struct Moves {
   u32x4_t x[kMoveUnroll];
