@@ -194,6 +194,7 @@ def _stream_handle(device: int) -> int:
 
 
 _current_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _stream_handle)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)  # where there are device tensors
 
 
 def lg_guard_params_default() -> GuardParams:
@@ -329,9 +330,8 @@ def _on(device: int, stream, layer=None):
     """The stream of a paged call, which runs on the current device: the map's and the layer's."""
     if layer is not None and layer.device != device:
         raise LGError("the layer's pages are on device %d, the page map on device %d" % (layer.device, device))
-    if torch.cuda.current_device() != device:
-        raise LGError("the page map is on device %d, the current device is %d" %
-                      (device, torch.cuda.current_device()))
+    if _current_device() != device:
+        raise LGError("the page map is on device %d, the current device is %d" % (device, _current_device()))
     return _current_raw_stream(device) if stream is None else _stream(stream)
 
 
@@ -474,6 +474,7 @@ def lg_paged_attend(layer: PagedLayer, m: PageMap, q, out, q_start, base, max_ch
 # 4-bit pages and rotary positions with several axes (include/lg_fp4.h).
 # ------------------------------------------------------------------------------------------------
 _NUMBER = {torch.float32: LG_F32, torch.bfloat16: LG_BF16}
+_I32, _F32 = torch.int32, torch.float32
 
 
 def _number(dtype, what):
@@ -514,15 +515,15 @@ def lg_rope_axes(sections: Sequence[int], order: int = LG_AXES_BLOCKS) -> torch.
 def lg_rope_append_axes(layer: PagedLayer, m: PageMap, q, k, v, inv_freq, rot_dim: int, interleaved, scale: float, axis,
                         coord, q_out, q_start, base, stream=None):
     """axis, coord: int32 [rot_dim / 2] and [axes][total], or None both (positions of the map)."""
-    dev, D, i32 = m.device, layer.head_dim, torch.int32
+    dev, D, B, half = m.device, layer.head_dim, m.batch, rot_dim // 2
     stream = _on(dev, stream, layer)
     x = q if q is not None else k
     if x is None or (k is None) != (v is None) or (q is None) != (q_out is None):
         raise LGError("lg_rope_append_axes: needs q with q_out, k with v, or all of them")
     total, dt = x.shape[0], x.dtype
     number = _number(dt, "lg_rope_append_axes")
-    qp = kp = vp = op = None
-    qs = ks = vs = 0
+    qp = kp = vp = op = fp = ap = cp = None
+    qs = ks = vs = n_axes = stride = 0
     if q is not None:
         qp, qs = _rows(q, layer.n_q_heads, D, dt, dev, "q")
         op = _need(q_out, dt, total * layer.n_q_heads * D, dev, "q_out")
@@ -531,35 +532,34 @@ def lg_rope_append_axes(layer: PagedLayer, m: PageMap, q, k, v, inv_freq, rot_di
             raise LGError("lg_rope_append_axes: needs as many rows of k and v as of q")
         kp, ks = _rows(k, layer.n_kv_heads, D, dt, dev, "k")
         vp, vs = _rows(v, layer.n_kv_heads, D, dt, dev, "v")
-    fp = None if rot_dim == 0 else _need(inv_freq, torch.float32, rot_dim // 2, dev, "inv_freq")
-    ap = cp = None
-    n_axes = 0
+    if half:
+        fp = _need(inv_freq, _F32, half, dev, "inv_freq")
     if coord is not None or axis is not None:
         if coord is None or axis is None or coord.dim() != 2 or coord.shape[1] < total:
             raise LGError("lg_rope_append_axes: needs axis and coord [axes][rows], or neither")
-        n_axes = coord.shape[0]
-        ap, cp = _need(axis, i32, rot_dim // 2, dev, "axis"), _need(coord, i32, n_axes * total, dev, "coord")
-    _check(_lib.lg_rope_append_axes(ctypes.byref(layer), ctypes.byref(m), number, qp, qs, kp, ks, vp, vs, fp, rot_dim,
-                                    int(bool(interleaved)), scale, ap, cp, 0 if coord is None else coord.shape[1], n_axes, op,
-                                    _need(q_start, i32, m.batch + 1, dev, "q_start"),
-                                    _need(base, i32, m.batch, dev, "base"), total, stream),
-           "lg_rope_append_axes")
+        n_axes, stride = coord.shape
+        ap, cp = _need(axis, _I32, half, dev, "axis"), _need(coord, _I32, 0, dev, "coord")
+    status = _lib.lg_rope_append_axes(ctypes.byref(layer), ctypes.byref(m), number, qp, qs, kp, ks, vp, vs, fp, rot_dim,
+                                      1 if interleaved else 0, scale, ap, cp, stride, n_axes, op,
+                                      _need(q_start, _I32, B + 1, dev, "q_start"), _need(base, _I32, B, dev, "base"), total, stream)
+    if status:
+        _check(status, "lg_rope_append_axes")
 
 
 def lg_page_unpack_fp4(layer: PagedLayer, m: PageMap, k_out, v_out, q_start, base, stream=None):
-    dev, i32 = m.device, torch.int32
+    dev, B = m.device, m.batch
     stream = _on(dev, stream, layer)
     x = k_out if k_out is not None else v_out
     if x is None:
         raise LGError("lg_page_unpack_fp4: needs k_out or v_out")
     total, dt = x.shape[0], x.dtype
     number, n = _number(dt, "lg_page_unpack_fp4"), total * layer.n_kv_heads * layer.head_dim
-    _check(_lib.lg_page_unpack_fp4(ctypes.byref(layer), ctypes.byref(m), number,
-                                   None if k_out is None else _need(k_out, dt, n, dev, "k_out"),
-                                   None if v_out is None else _need(v_out, dt, n, dev, "v_out"),
-                                   _need(q_start, i32, m.batch + 1, dev, "q_start"),
-                                   _need(base, i32, m.batch, dev, "base"), total, stream),
-           "lg_page_unpack_fp4")
+    status = _lib.lg_page_unpack_fp4(ctypes.byref(layer), ctypes.byref(m), number,
+                                     None if k_out is None else _need(k_out, dt, n, dev, "k_out"),
+                                     None if v_out is None else _need(v_out, dt, n, dev, "v_out"),
+                                     _need(q_start, _I32, B + 1, dev, "q_start"), _need(base, _I32, B, dev, "base"), total, stream)
+    if status:
+        _check(status, "lg_page_unpack_fp4")
 
 
 def lg_paged_attend_fp4_workspace(layer: PagedLayer, m: PageMap, dtype, total: int, max_chunk: int) -> int:
@@ -570,19 +570,19 @@ def lg_paged_attend_fp4_workspace(layer: PagedLayer, m: PageMap, dtype, total: i
 
 def lg_paged_attend_fp4(layer: PagedLayer, m: PageMap, q, out, q_start, base, max_chunk: int, window: int, n_sink: int,
                         suffix_w, lse, suffix_mass, conf, workspace, stream=None):
-    dev, B, dt, i32, f32 = m.device, m.batch, q.dtype, torch.int32, torch.float32
+    dev, B, dt, total = m.device, m.batch, q.dtype, q.shape[0]
     stream = _on(dev, stream, layer)
-    total, n = q.shape[0], q.shape[0] * layer.n_q_heads
+    n = total * layer.n_q_heads
     ws, size = _bytes(workspace, dev, "workspace")
-    _check(_lib.lg_paged_attend_fp4(
+    status = _lib.lg_paged_attend_fp4(
         ctypes.byref(layer), ctypes.byref(m), _number(dt, "lg_paged_attend_fp4"), _need(q, dt, n * layer.head_dim, dev, "q"),
-        _need(out, dt, n * layer.head_dim, dev, "out"), _need(q_start, i32, B + 1, dev, "q_start"),
-        _need(base, i32, B, dev, "base"), total, max_chunk, window, n_sink,
-        None if suffix_w is None else _need(suffix_w, i32, B, dev, "suffix_w"),
-        _need(lse, f32, n, dev, "lse"),
-        None if suffix_mass is None else _need(suffix_mass, f32, n, dev, "suffix_mass"),
-        None if conf is None else _need(conf, f32, B, dev, "conf"), ws, size, stream),
-        "lg_paged_attend_fp4")
+        _need(out, dt, n * layer.head_dim, dev, "out"), _need(q_start, _I32, B + 1, dev, "q_start"),
+        _need(base, _I32, B, dev, "base"), total, max_chunk, window, n_sink,
+        None if suffix_w is None else _need(suffix_w, _I32, B, dev, "suffix_w"), _need(lse, _F32, n, dev, "lse"),
+        None if suffix_mass is None else _need(suffix_mass, _F32, n, dev, "suffix_mass"),
+        None if conf is None else _need(conf, _F32, B, dev, "conf"), ws, size, stream)
+    if status:
+        _check(status, "lg_paged_attend_fp4")
 
 
 def params_from_dict(d) -> GuardParams:
