@@ -47,8 +47,8 @@ lg_status lg_rope_axes(int32_t n_axes, const int32_t *sections, int32_t order, i
  * As lg_rope_append, but
  *   - pair j of token i of sequence b, row r = q_start[b] + i, turns by a_j = p inv_freq[j] with p =
  *     coord[axis[j]][r]: the token's place in time, height and width, say. With n_axes = 0, p = pos[b][slot] for all.
- *     Masks and windows go by pos as ever. cos and sin are formed in double, scaled and rounded once to float32, as
- *     the products and their sum are.
+ *     Masks and windows go by pos as ever. cos and sin are formed in double, scaled and rounded once to float32; for 4-bit
+ *     keys the products with them and their sum are rounded to float32 one by one.
  *   - dtype is the type of q, k, v and q_out (LG_F32 or LG_BF16). A layer of LG_FP4 takes both; keys are rounded to 4 bits
  *     from the float32 rotation, values from what they are. Any other layer takes its own type (LG_ERR_UNSUPPORTED).
  *   - keys and values alone: q and q_out may both be NULL (k and v are then given).

@@ -287,9 +287,8 @@ __global__ __launch_bounds__(kAxesThreads) void page_unpack(UnpackArgs a) {
   __shared__ int2 place[kUnpackRows];  // page (-1: nothing to read) and row in it
   const int rows = 1 << a.log_rows, r0 = blockIdx.x * rows, tid = threadIdx.x;
   if (tid < 64) {
-    int b = seq_of_row(a.q_start, a.map.B, r0);
     const int r = r0 + min(tid, rows - 1);
-    while (b < a.map.B && a.q_start[b + 1] <= r) ++b;  // rows ascend, as sequences do
+    const int b = seq_behind(a.q_start, a.map.B, seq_of_row(a.q_start, a.map.B, r0), r);  // rows ascend, as sequences do
     int page = -1, slot = 0;
     if (b < a.map.B && r < a.total) {
       const Chunk c = chunk_of(a.q_start, b, a.total);

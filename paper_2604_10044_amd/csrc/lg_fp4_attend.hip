@@ -543,11 +543,11 @@ __device__ __forceinline__ void few_body(const PagedAttendArgs& a, Job job, char
     for (int i = 0; i < kPairs; ++i) *(f32x2*)(a.po + (split0 + row) * D + job.d0 + 2 * (kParts * i + share)) = x[i];
     return;
   }
-  const float inv = 1.f / L;
+  const float inv = L == 0.f ? 0.f : 1.f / L;  // without weight x is 0, or NaN by a group that stands for it
   T* dst = (T*)a.out + row * D + job.d0;
 #pragma unroll
   for (int i = 0; i < kPairs; ++i) {
-    const float y0 = L == 0.f ? 0.f : x[i][0] * inv, y1 = L == 0.f ? 0.f : x[i][1] * inv;
+    const float y0 = x[i][0] * inv, y1 = x[i][1] * inv;
     if constexpr (sizeof(T) == 4)
       *(f32x2*)(dst + 2 * (kParts * i + share)) = f32x2{y0, y1};
     else
@@ -798,8 +798,8 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
   if (idle) return;
   l += other_half(l);
   sfx += other_half(sfx);
-  const float inv = l > 0.f || l != l ? 1.f / l : 0.f;  // no slot seen: 0
-  const float mass = l == 0.f ? 0.f : sfx * inv;
+  const float inv = l == 0.f ? 0.f : 1.f / l;  // without weight O is 0, or NaN by a group that stands for it
+  const float mass = sfx * inv;
   if (a.ns == 1 && a.conf != nullptr) raise_conf(a.conf + job.b, mass, tok == job.rows / a.G - 1);
   if (!live) return;
   if (a.ns > 1) {
@@ -819,7 +819,7 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
     for (int i = 0; i < 4; ++i) {
       float x[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = l == 0.f ? 0.f : O[d][4 * i + e] * inv;
+      for (int e = 0; e < 4; ++e) x[e] = O[d][4 * i + e] * inv;
       if constexpr (sizeof(T) == 4)
         *(f32x4*)(dst + 32 * d + 8 * i + 4 * part) = f32x4{x[0], x[1], x[2], x[3]};
       else
@@ -913,8 +913,7 @@ __global__ __launch_bounds__(kPagedThreads) void fp4_join(PagedAttendArgs a) {
   };
   load(g);
   // the sequences of the workgroup's first row, and from there on those that end before this row
-  int b = seq_of_row(a.q_start, a.map.B, (int)(first / a.Hq));
-  while (b < a.map.B && a.q_start[b + 1] <= r) ++b;
+  const int b = seq_behind(a.q_start, a.map.B, seq_of_row(a.q_start, a.map.B, (int)(first / a.Hq)), r);
   const bool some = b < a.map.B;
   const Chunk c = some ? chunk_of(a.q_start, b, a.total) : Chunk{0, 0};
   const int base = some ? a.base[b] : -1;
@@ -945,8 +944,8 @@ __global__ __launch_bounds__(kPagedThreads) void fp4_join(PagedAttendArgs a) {
   }
   const bool live = g == 0 && first + in < rows && r >= c.first && r < c.first + c.n && c.n <= a.max_chunk && base >= 0 &&
                     base <= a.map.cap - c.n;
-  const float inv = 1.f / L;
-  const float mass = L == 0.f ? 0.f : SF * inv;
+  const float inv = L == 0.f ? 0.f : 1.f / L;
+  const float mass = SF * inv;
   if (a.conf != nullptr) {  // one atomic a workgroup and token
     const int at = r - (int)(first / a.Hq);  // below kRows: a token has a row at least
     const bool newest = live && r == c.first + c.n - 1;
@@ -958,7 +957,7 @@ __global__ __launch_bounds__(kPagedThreads) void fp4_join(PagedAttendArgs a) {
   }
   if (!live) return;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = L == 0.f ? 0.f : x[e] * inv;
+  for (int e = 0; e < 4; ++e) x[e] *= inv;
   T* dst = (T*)a.out + row * D + 4 * lane;
   if constexpr (sizeof(T) == 4)
     *(f32x4*)dst = x;

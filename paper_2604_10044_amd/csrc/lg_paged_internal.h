@@ -56,6 +56,21 @@ __device__ __forceinline__ int seq_of_row(const int32_t* q_start, int B, int r) 
   return b;
 }
 
+// The sequence of a row at or behind those of sequence b, each lane for itself: steps that double, then halves, since
+// thousands of sequences without rows may lie between.
+__device__ __forceinline__ int seq_behind(const int32_t* q_start, int B, int b, int r) {
+  int lo = b, step = 1;  // the answer is lo or more
+  while (lo < B && q_start[min(lo + step, B)] <= r) {
+    lo = min(lo + step, B);
+    step *= 2;
+  }
+  for (int hi = min(lo + step - 1, B); lo < hi;) {
+    const int mid = (lo + hi) >> 1;
+    if (q_start[mid + 1] <= r) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+
 // 4-bit layers (lg_fp4.h): bytes of a row's values, of its exponents, and of the block of a page and a head.
 constexpr int kFp4Group = 32;  // values of one exponent
 __host__ __device__ __forceinline__ constexpr int fp4_row(int D) { return D / 2; }

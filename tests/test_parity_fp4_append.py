@@ -352,6 +352,37 @@ def test_unpack_of_many_slots(total):
         np.testing.assert_array_equal(o.double().cpu().numpy(), want)
 
 
+def test_unpack_over_thousands_of_empty_sequences():
+    """The rows of a workgroup belong to sequences far apart, or next to each other."""
+    from paper_2604_10044_amd import lg
+    B, ps, D, r = 40000, 16, 64, np.random.RandomState(3)
+    lens = np.zeros(B, np.int64)
+    some = np.unique(np.concatenate([r.randint(0, 3000, 700), r.randint(37000, B, 700), np.arange(2990, 3000)]))
+    lens[some] = r.choice([1, 2, 3, 15, 16, 17, 60], len(some))
+    total = int(lens.sum())
+    assert total > 16 * 1024  # 16 slots a workgroup
+    P = -(-int(lens.max()) // ps)
+    P_of = -(-lens // ps)
+    i32 = lambda y: torch.as_tensor(np.asarray(y, np.int32), device="cuda")  # noqa: E731
+    pages, start = int(P_of.sum()), np.concatenate([[0], np.cumsum(lens)])
+    order, off = r.permutation(pages), np.concatenate([[0], np.cumsum(P_of)])
+    table = np.full((B, P), -1)
+    for b in some:
+        table[b, :P_of[b]] = order[off[b]:off[b + 1]]
+    table = i32(table)
+    x = r.randint(0, 256, (pages, 1, lg.fp4_page_bytes(ps, D))).astype(np.uint8)
+    x[..., ps * D // 2:] = 127
+    d = torch.as_tensor(x, device="cuda")
+    layer = lg.paged_layer_fp4(d, d.clone(), 1, ps, D)
+    m = lg.page_map(table, torch.zeros(B, P * ps, dtype=torch.int32, device="cuda"), i32(lens), i32(np.ones(pages)), ps)
+    o = torch.full((total, 1, D), 9.0, device="cuda")
+    lg.lg_page_unpack_fp4(layer, m, o, None, i32(start), i32(np.zeros(B)))
+    seq = np.repeat(np.arange(B), lens)
+    slot = np.arange(total) - start[seq]
+    page = order[off[seq] + slot // ps]
+    np.testing.assert_array_equal(o.double().cpu().numpy(), fp4.values(*fp4.unpack(x, ps, D))[page, :, slot % ps])
+
+
 @pytest.mark.parametrize("bits", [4, 16])
 def test_many_sequences(bits):
     """More sequences than a wave looks at together, some without tokens."""

@@ -325,6 +325,23 @@ def test_nan_of_a_vanishing_weight(dtype):
             assert np.isfinite(out[..., :32]).all()
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_nan_without_any_weight(dtype):
+    """Queries of infinity before keys below 0: every score is -inf and no slot has weight. 0, but NaN in the 32 values of a
+    group that stands for it; in a chunk, in a step of one workgroup and in one of several splits."""
+    for hkv, have, n in ((1, 0, 128), (2, 50, 1), (2, 3000, 1), (2, 3000, 40)):
+        a = Attend4(dtype, 64, hkv, hkv, 16, [have], [n], seed=26, holes=False)
+        a.q.fill_(float("inf"))
+        a.k.fill_(-1.0)
+        a.alloc()
+        a.exponents(1)[int(a.table_h[0, 0]), :, 10, 1] = 255
+        a.call()
+        out, lse, sm, _ = a.results()
+        first = max(0, 10 - have)  # the first token that sees slot 10
+        assert (lse[:n] == -np.inf).all() and (sm[:n] == 0).all()
+        assert (out[:n, :, :32] == 0).all() and (out[:first] == 0).all() and np.isnan(out[first:n, :, 32:]).all()
+
+
 @pytest.mark.parametrize("dtype, D, hq, hkv", [(BF, 128, 8, 2), (BF, 64, 6, 6), (F32, 128, 4, 1), (F32, 64, 4, 4)])
 @pytest.mark.parametrize("chunk", [1, 3, 70])
 @pytest.mark.parametrize("window, sinks", [(100, 4), (2500, 40), (9000, 0), (30000, 600)])
@@ -416,6 +433,16 @@ def test_many_sequences(B, dtype):
     a = Attend4(dtype, 64, 4, 2, 16, [(b * 13) % 50 for b in range(B)], n, seed=19)
     a.call()
     a.check()
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_splits_of_a_sequence_behind_empty_ones(dtype):
+    """A workgroup that joins splits has rows of two sequences, with many of no rows, or a few, between them."""
+    for empty in (1, 2, 3, 7, 60):
+        n = [3] + [0] * empty + [2, 0, 1]
+        a = Attend4(dtype, 64, 1, 1, 16, [2000] + [5] * empty + [1900, 3, 2000], n, seed=27)
+        a.call()
+        a.check()
 
 
 @pytest.mark.parametrize("dtype", [BF, F32])
