@@ -22,7 +22,9 @@
 // exponents of a row in one load, spread by permutes (18.4 / 139); tiles of 64 slots (15.7 against 16.0 / 103 against 101); 4 waves
 // a workgroup (18.3 against 16.0). Chunks: the scores of both blocks of 32 keys side by side, or the next tile's conversion among
 // them (4096 tokens 510 to 640: registers); two teams of four waves a workgroup that share out the tiles (8 sequences of 128 tokens,
-// window 1024, 28.5 against 31.4, the mixed step 51 against 46: one barrier keeps the teams in step).
+// window 1024, 28.5 against 31.4, the mixed step 51 against 46: one barrier keeps the teams in step); a higher priority for a wave
+// in its matrix instructions (4096 tokens 422 to 426 against 425, in float32 1105 to 1153 against 1084) or in its exponentials (432); all
+// exponentials before the second product (433).
 #include "lg_fp4.h"
 #include "lg_paged_attend.h"
 
