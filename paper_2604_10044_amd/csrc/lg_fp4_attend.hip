@@ -24,7 +24,8 @@
 // them (4096 tokens 510 to 640: registers); two teams of four waves a workgroup that share out the tiles (8 sequences of 128 tokens,
 // window 1024, 28.5 against 31.4, the mixed step 51 against 46: one barrier keeps the teams in step); a higher priority for a wave
 // in its matrix instructions (4096 tokens 422 to 426 against 425, in float32 1105 to 1153 against 1084) or in its exponentials (432); all
-// exponentials before the second product (433).
+// exponentials before the second product (433); a maximum for each 32 keys, so that the second scores run beside the first
+// exponentials (445 against 434, with the scheduler's order forced 452 to 463).
 #include "lg_fp4.h"
 #include "lg_paged_attend.h"
 
