@@ -501,3 +501,26 @@ def test_binding_refuses():
             lg.lg_page_unpack_fp4(s.layer, s.map, a, b, s.q_start, s.base)
     s.call(f, 64, axis=axis)
     s.check(f, 64, False, 1.0, was)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("D", [64, 128])
+def test_unpack_of_every_exponent_and_code(dtype, D):
+    """Each of the 16 codes beside each exponent byte: the values are exact in both types, those below the least normal number
+    too (2^-128 is the least), and bytes above 252 stand for NaN."""
+    from paper_2604_10044_amd import lg
+    ps, n_pages = 256, D // 32
+    codes, exps = np.zeros((n_pages, 1, ps, D), np.uint8), np.zeros((n_pages, 1, ps, D // 32), np.uint8)
+    for p in range(n_pages):  # the groups of a row have bytes far apart
+        exps[p, 0] = (np.arange(ps)[:, None] + 64 * np.arange(D // 32) + p) % 256
+        codes[p, 0] = (np.arange(D) + p) % 16
+    pages = torch.as_tensor(fp4.pack(codes, exps), device="cuda")
+    layer = lg.paged_layer_fp4(pages, pages.clone(), 1, ps, D)
+    i32 = lambda x: torch.as_tensor(np.asarray(x, np.int32), device="cuda")  # noqa: E731
+    m = lg.page_map(i32(np.arange(n_pages)[None]), i32(np.arange(n_pages * ps)[None]), i32([n_pages * ps]), i32(np.ones(n_pages)), ps)
+    k, v = (torch.full((n_pages * ps, 1, D), 9.0, device="cuda", dtype=dtype) for _ in range(2))
+    lg.lg_page_unpack_fp4(layer, m, k, v, i32([0, n_pages * ps]), i32([0]))
+    want = fp4.values(codes, exps)[:, 0].reshape(-1, 1, D)
+    assert 0 < np.nanmin(np.abs(want)[want != 0]) == 2.0 ** -128
+    for x in (k, v):
+        np.testing.assert_array_equal(x.double().cpu().numpy(), want)

@@ -515,3 +515,44 @@ def test_binding_refuses():
         lg.lg_paged_attend(a.layer, a.map, a.q, a.out, a.q_start, a.base, 3, 0, 0, None, a.lse, None, None, a.ws)
     a.call()
     a.check()
+
+
+@pytest.mark.parametrize("dtype,D,n", [(BF, 128, [1, 4]), (BF, 64, [1, 1]), (BF, 128, [40, 1]), (BF, 64, [70, 2]), (F32, 128, [2, 1]),
+                                       (F32, 64, [1, 3]), (F32, 128, [40, 1]), (F32, 64, [1, 50])])
+@pytest.mark.parametrize("keys,values", [((0, 1, 2), ()), ((248, 250, 252), ()), ((), (0, 1, 2)), ((), (236, 238, 240)), ((0, 1), (0, 2))])
+def test_exponents_at_the_ends(dtype, D, n, keys, values):
+    """Groups with the least and the largest units, and queries that bring the scores to ordinary size. Queries are bfloat16
+    numbers. Products and sums of values below 2^-126 are off by half a step of the least numbers, 2^-149 in float32: three
+    terms of e slots, their sums and the scaling; a bfloat16 result by half of 2^-133."""
+    a = Attend4(dtype, D, 4, 2, 16, [70, 10], n, seed=31, holes=False)
+    for which, units in ((0, keys), (1, values)):
+        if units:
+            e = a.exponents(which)
+            e.copy_(torch.as_tensor(a.r.choice(units, tuple(e.shape)).astype(np.uint8), device="cuda"))
+            x = (a.k, a.v)[which]
+            x.copy_(torch.as_tensor(fp4.values(*fp4.unpack(a.bytes[which].cpu().numpy(), a.ps, a.D))).to(x.dtype))
+    if keys:  # keys of some two units: queries of half of one over the unit
+        a.q.copy_((a.q.double().clamp(-4, 4) * 2.0 ** (125 - max(keys))).to(BF).to(dtype))
+    a.call()
+    out, lse, sm, conf = a.results()
+    assert np.isfinite(out).all() and np.isfinite(lse).all()
+    k, v, q = (x.double().cpu().numpy() for x in (a.k, a.v, a.q))
+    G = a.hq // a.hkv
+    half, w = (2.0 ** -8, 2.0 ** -8) if dtype is BF else (2.0 ** -24, 0.0)
+    for b in range(len(n)):
+        for i in range(n[b]):
+            e, row = a.have[b] + i + 1, a.start_h[b] + i
+            slots = np.arange(e)
+            page = a.table_h[b, slots // a.ps]
+            for h in range(a.hkv):
+                kk, vv = (x[page, h, slots % a.ps] for x in (k, v))
+                o, ls, ms, av, big = (x[0] for x in paged.attend(q[row, h * G:(h + 1) * G][None], kk, vv, a.pos_h[b, :e], e - 1, 0, 0,
+                                                                 int(a.sw_h[b])))
+                assert 0.5 < big.max() < 200
+                err = ((D + 8) * big + 4 * e / 32 + 144) * 2.0 ** -24
+                least = (3 * e + 8) * 2.0 ** -149 + (2.0 ** -134 if dtype is BF else 0)
+                tol = ((2 * err[:, None] + w) * av) * (1 + half) + half * np.abs(o) + e * 2.0 ** -124 * np.abs(vv).max() + least
+                heads = slice(h * G, (h + 1) * G)
+                assert (np.abs(out[row, heads] - o) <= tol).all(), (b, i, h, np.abs(out[row, heads] - o).max(), tol.min())
+                assert (np.abs(lse[row, heads] - ls) <= err + 2.0 ** -22 * (np.abs(ls) + big)).all(), (b, i, h)
+                assert (np.abs(sm[row, heads] - ms) <= 2 * err * ms + e * 2.0 ** -126).all(), (b, i, h)
