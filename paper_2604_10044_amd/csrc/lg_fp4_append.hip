@@ -118,6 +118,15 @@ __device__ __forceinline__ Eight rotated_eight(const T* src, int u, int rot, con
   return y;
 }
 
+// The fraction of a turn, at most half a turn in size, of the angle p f: within 2^-53 of a turn at any p. The product has up to
+// 55 bits and its whole turns up to 31, so it is carried as two doubles, as is 1 / (2 pi); the whole turns leave in a fused
+// step (with one double each, the angle at 2^30 is off by 2e-7, 3.5 units of a float32 sine).
+__device__ __forceinline__ double fraction_of_turn(int p, float f) {
+  constexpr double kTurn = 0x1.45f306dc9c883p-3, kTurnRest = -0x1.6b01ec5417056p-57;  // together 1 / (2 pi)
+  const double x = (double)p * (double)f, rest = fma((double)p, (double)f, -x);
+  return fma(x, kTurn, -rint(x * kTurn)) + fma(x, kTurnRest, rest * kTurn);
+}
+
 // A workgroup a token. Its rot_dim / 2 angles are formed once, in double (positions and coordinates reach 2^31, and what
 // is rounded to 4 bits shall not depend on the last bits of a sine): a thread each. The
 // threads then walk the token's keys and values (8 values each, so that four lanes are a group) and its queries.
@@ -138,9 +147,8 @@ __global__ __launch_bounds__(kAxesThreads) void append_axes(AxesArgs a) {
   if (tid < half) {
     const int p = a.n_axes > 0 ? a.coord[min(max(a.axis[tid], 0), a.n_axes - 1) * a.coord_stride + r]
                                : a.map.pos[(size_t)b * a.map.cap + slot];
-    const double turns = (double)p * (double)a.inv_freq[tid] * 0.15915494309189533577;  // 1 / (2 pi)
     double s, co;
-    sincospi(2. * (turns - rint(turns)), &s, &co);
+    sincospi(2. * fraction_of_turn(p, a.inv_freq[tid]), &s, &co);
     cs[tid] = (float)((double)a.scale * co);
     cs[64 + tid] = (float)((double)a.scale * s);
   }

@@ -524,3 +524,31 @@ def test_unpack_of_every_exponent_and_code(dtype, D):
     assert 0 < np.nanmin(np.abs(want)[want != 0]) == 2.0 ** -128
     for x in (k, v):
         np.testing.assert_array_equal(x.double().cpu().numpy(), want)
+
+
+@pytest.mark.parametrize("axes", [0, 3])
+@pytest.mark.parametrize("far", [0, 2 ** 20, 2 ** 27, 2 ** 30 - 10000, 2 ** 31 - 10000])
+def test_sines_are_rounded_once_at_any_distance(far, axes):
+    """Pairs (1, 0) become (scale cos a, scale sin a) themselves, which are rounded once to float32: half a step of 2^-24
+    beside what double leaves: the fraction of a turn is off by 2^-53 of one at most, 2 pi 2^-53, the sine and its product with
+    scale by 2^-51 more. A coordinate times a frequency has up to 31 + 24 bits, so the fraction is not in its rounded product."""
+    if axes == 0:
+        far = min(far, 2 ** 30 - 10000)
+    s = Step(F32, 32, 128, 4, 2, 32, [3, 0], [37, 41], axes=axes, seed=13, far=far)
+    for x in (s.q, s.kn):
+        x[..., :64], x[..., 64:] = 1, 0
+    if axes:
+        s.coord_h = np.random.RandomState(far % 1000).randint(far, far + 9000, s.coord_h.shape)
+        s.coord_h[1] *= -1
+        s.coord = s.i32(s.coord_h)
+    was, freq = s.state(), _freq(128)
+    axis = s.lg.lg_rope_axes([20, 20, 24], s.lg.LG_AXES_TURNS).numpy() if axes else None
+    s.call(freq, 128, scale=1.25, axis=axis)
+    got, T = s.state(), sum(s.n)
+    coord = s.coord_h[:, :T] if axes else np.concatenate([s.pos_h[b, h:h + n] for b, (h, n) in enumerate(zip(s.have, s.n))])[None]
+    want, _ = fp4.rope_axes(was[3][:T, :6], coord, s.axis_h, freq.cpu().numpy(), 128, False, 1.25)
+    tol = 2.0 ** -24 * np.abs(want) + 1.25 * (2 * np.pi * 2.0 ** -53 + 2.0 ** -51)
+    assert (np.abs(got[2][:T] - want[:, :4]) <= tol[:, :4]).all(), np.abs(got[2][:T] - want[:, :4]).max()
+    slots = np.concatenate([h + np.arange(n) for h, n in zip(s.have, s.n)])
+    k = got[0][s.table_h[np.repeat(np.arange(2), s.n), slots // 32], :, slots % 32]
+    assert (np.abs(k - want[:, 4:]) <= tol[:, 4:]).all()
