@@ -14,8 +14,10 @@
  * four bits: sign s (the highest), two bits of exponent, one of fraction, for 0, 0.5, 1, 1.5, 2, 3, 4 and 6 units. Each is a
  * bfloat16 number exactly. Appending 32 values of largest magnitude m takes the smallest unit with m <= 6 u,
  * within 2^-125 .. 2^125 (x = 2 .. 252), and rounds each value to the nearest code, ties to the code with fraction 0;
- * what lies beyond 6 u (m > 6 2^125 alone) becomes 6 u. So a value moves by at most u (m / 3 at most), by u / 4 where
- * it is at most 2 u. 32 values of which one is infinite or NaN get x = 255; they, and those of any x above 252, stand for NaN.
+ * what lies beyond 6 u (m > 6 2^125 alone) becomes 6 u. So a value moves by at most u / 4 where it is at most 2 u, by u / 2 up
+ * to 4 u and by u up to 6 u; u is below m / 3 where m > 3 2^-125. At the ends, a value of a group with m <= 3 2^-125 moves by at
+ * most 2^-126 and may become 0, and one beyond 6 2^125 moves by less than 2^126. 32 values of which one is infinite or NaN get
+ * x = 255; they, and those of any x above 252, stand for NaN.
  *
  * Layout. lg_paged_layer with dtype LG_FP4: k, v [n_pages][n_kv_heads][page_size (head_dim / 2 + head_dim / 32)]
  * bytes. The block of a page and a head is page_size rows of head_dim / 2 bytes, value 2 i in the low half of byte i

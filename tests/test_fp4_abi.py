@@ -236,3 +236,23 @@ def test_the_model_of_rows():
     assert b.shape == (50, 2, 16 * 68)
     for p, q in zip(fp4.unpack(b, 16, 128), (codes, exps)):
         np.testing.assert_array_equal(p, q)
+
+
+def test_how_far_a_value_moves():
+    """The bounds that lg_fp4.h gives: in units between its ends, and at both ends, where a third of the largest value is none."""
+    r = np.random.RandomState(2)
+    x = r.uniform(-1, 1, (4000, 64)) * 2.0 ** r.uniform(-140, 128, (4000, 1))
+    x[:32] = 2.0 ** r.randint(-149, -120, (32, 64)) * r.choice([-1, 1], (32, 64))
+    x[32, :4], x[33, :4] = [3.4e38, -3.4e38, 1e38, 5e-324], [1e-45, 2.0 ** -127, 2.0 ** -126, 0]
+    top = np.repeat(np.abs(x).reshape(4000, 2, 32).max(-1), 32, -1)
+    codes, exps = fp4.encode(x)
+    unit = np.repeat(2.0 ** (exps - 127.0), 32, -1)
+    size, moved = np.abs(x), np.abs(fp4.values(codes, exps) - x)
+    inside, small, large = size <= 6 * unit, top <= 3 * 2.0 ** -125, size > 6 * unit
+    for most, share in ((2, 4), (4, 2), (6, 1)):
+        at = inside & (size <= most * unit)
+        assert (moved[at] <= (unit / share)[at]).all()
+    assert (unit < top / 3)[~small].all() and (moved[~small & inside] < (top / 3)[~small & inside]).all()
+    assert (moved[small] <= 2.0 ** -126).all() and (moved[small] > (top / 3)[small]).any()
+    assert (top[large] > 6 * 2.0 ** 125).all() and (moved[large] < 2.0 ** 126).all() and (moved[large] > unit[large]).any()
+    assert ((fp4.values(codes, exps) == 0) & (x != 0) & small).any()
