@@ -4,6 +4,8 @@ import numpy as np
 import pytest
 import torch
 
+from oracle import paged
+
 pytestmark = pytest.mark.gpu
 
 B, L, HQ, HKV, D, PS, P = 3, 2, 8, 2, 64, 16, 8
@@ -259,3 +261,47 @@ def test_out_of_pages_marks_the_sequence():
     a.guard(_tokens(), _i32([32, 32, 0]))
     assert a.decision[:, a.lg.ATTEND_ERROR_COL].tolist() == [0, 1, 1]
     assert torch.equal(before, a.read(0, [0, 32, 0])[0])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_guarded_loop_rows_against_64_bits(dtype):
+    """Every row of a guarded loop's steps against attention in 64 bits on what its pages hold: chunks of prompts, then decode
+    steps between prunes. The bounds are those of test_parity_fp4_attend.py: of each weight (2^-8 in bfloat16 chunks, 2^-16 in steps
+    of few rows, 0 in float32) times sum alpha |v|, half a step of the result, and float32 sums."""
+    a, G = Loop(dtype, True), HQ // HKV
+    r = np.random.RandomState(5)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    tokens, t, prunes, most = _tokens(), np.full(B, -1), 0, 0.0
+    for step, n in enumerate([[30, 20, 1], [20, 0, 32]] + [[1, 1, 1]] * 90):
+        t = t + n
+        q_start = np.concatenate([[0], np.cumsum(n)])
+        got = a.step(torch.randn(L, sum(n), HQ + 2 * HKV, D, generator=g, device="cuda").to(dtype), _coord(r, t, n), _i32(q_start), _i32(t), max(n))
+        if step < 2 or step % 9 == 0:
+            base, pos, sw = (x.cpu().numpy() for x in (a.base, a.pos, a.sw))
+            full = base + n
+            at = np.concatenate([[0], np.cumsum(full)])
+            for l, (q, out, lse, sm) in enumerate(got):
+                k, v = (x.double().cpu().numpy() for x in a.read(l, full))
+                q, out, lse, sm = (x.double().cpu().numpy() for x in (q, out, lse, sm))
+                for b in range(B):
+                    if n[b] == 0:
+                        continue
+                    rows, slots = slice(q_start[b], q_start[b + 1]), slice(at[b], at[b + 1])
+                    for h in range(HKV):
+                        heads = slice(h * G, (h + 1) * G)
+                        o, ls, ms, av, big = paged.attend(q[rows, heads], k[slots, h], v[slots, h], pos[b, :full[b]], base[b], 0, 0, int(sw[b]))
+                        err = ((D + 8) * big + 4 * full[b] / 32 + 144) * 2.0 ** -24
+                        half, w = (2.0 ** -8, 2.0 ** -8 if n[b] * G > 32 else 2.0 ** -16) if dtype is torch.bfloat16 else (2.0 ** -24, 0.0)
+                        tol = (2 * err[..., None] + w) * av * (1 + half) + half * np.abs(o) + full[b] * 2.0 ** -124 * np.abs(v).max()
+                        most = max(most, float((tol.max(-1) / av.max(-1)).max()))
+                        what = (step, l, b, h)
+                        assert (np.abs(out[rows, heads] - o) <= tol).all(), what
+                        assert (np.abs(lse[rows, heads] - ls) <= err + 2.0 ** -22 * (np.abs(ls) + big)).all(), what
+                        assert (np.abs(sm[rows, heads] - ms) <= 2 * err * ms + full[b] * 2.0 ** -126).all(), what
+        if step < 2:
+            a.conf.zero_()
+            continue
+        a.guard(tokens, _i32(t))
+        torch.cuda.synchronize()
+        prunes += int((a.new_len >= 0).sum())
+    assert prunes >= 4 and most < 2.0 ** -6  # beside the row's largest sum alpha |v|: a value too many or too few would show
