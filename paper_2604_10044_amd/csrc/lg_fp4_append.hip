@@ -27,12 +27,12 @@ struct AxesArgs {
 constexpr int kAxesThreads = 256;
 
 // 8 values of a head as float32
-struct Eight {
+struct Values {
   float x[8];
 };
 template <typename T>
-__device__ __forceinline__ Eight load_eight(const T* src) {
-  Eight y;
+__device__ __forceinline__ Values load_values(const T* src) {
+  Values y;
   constexpr int E = 16 / sizeof(T);
 #pragma unroll
   for (int i = 0; i < 8 / E; ++i) {
@@ -53,7 +53,7 @@ __device__ __forceinline__ uint32_t max_of_four(uint32_t x) {
 // The codes of a lane's 8 values and the exponent byte of the group that four lanes hold. With the bits of m as
 // exponent and fraction, m <= 1.5 2^(x - 127) exactly when the fraction is at most 0x400000: the sum below carries
 // otherwise, and u is 2^-2 of that power.
-__device__ __forceinline__ uint32_t encode(const Eight& y, uint32_t* exponent) {
+__device__ __forceinline__ uint32_t encode(const Values& y, uint32_t* exponent) {
   uint32_t m = 0;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(y.x[i]) & 0x7fffffffu);
@@ -75,11 +75,11 @@ __device__ __forceinline__ uint32_t encode(const Eight& y, uint32_t* exponent) {
 // Values 8 u .. 8 u + 7 of a rotated head. The products and sums are rounded one by one, as a program that multiplies and
 // adds would: a value next to the middle of two codes then falls to the same side.
 template <typename T, int M, bool ILV>
-__device__ __forceinline__ Eight rotated_eight(const T* src, int u, int rot, const float* cs) {
+__device__ __forceinline__ Values rotated_eight(const T* src, int u, int rot, const float* cs) {
 #pragma clang fp contract(off)
   const int half = rot / 2, i0 = 8 * u;
   const float* sn = cs + 64;
-  Eight y = load_eight(src + i0);
+  Values y = load_values(src + i0);
   if constexpr (M == kRopePairs) {
     if (i0 < rot) {
 #pragma unroll
@@ -94,7 +94,7 @@ __device__ __forceinline__ Eight rotated_eight(const T* src, int u, int rot, con
     if (i0 < rot) {
       const bool low = i0 < half;
       const int j = low ? i0 : i0 - half;
-      const Eight z = load_eight(src + (low ? i0 + half : j));
+      const Values z = load_values(src + (low ? i0 + half : j));
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         const float c = cs[j + e], s = sn[j + e];
@@ -165,7 +165,7 @@ __global__ __launch_bounds__(kAxesThreads) void append_axes(AxesArgs a) {
         const bool is_k = i < nk;
         const int x = is_k ? i : i - nk, h = x / ue, u = x - h * ue;
         const T* src = is_k ? (const T*)a.k + r * a.k_stride + h * a.D : (const T*)a.v + r * a.v_stride + h * a.D;
-        const Eight y = is_k ? rotated_eight<T, M, ILV>(src, u, a.rot, cs) : load_eight(src + 8 * u);
+        const Values y = is_k ? rotated_eight<T, M, ILV>(src, u, a.rot, cs) : load_values(src + 8 * u);
         uint32_t exponent;
         const uint32_t codes = encode(y, &exponent);
         char* at = (char*)(is_k ? a.pk : a.pv) + ((size_t)page * a.Hkv + h) * block;

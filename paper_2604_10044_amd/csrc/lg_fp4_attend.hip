@@ -581,7 +581,7 @@ struct Many {
 // Order for the scheduler: the 8 reads of LDS and 8 matrix instructions of a tile's scores at head_dim 64, the reads 4 ahead
 // (4096 tokens behind 4096, 32 / 8 heads: 298 us left to itself, 280 so; at head_dim 128 431 and 435, in float32 1081 and
 // 1123).
-__device__ __forceinline__ void schedule_scores() {
+__device__ __forceinline__ void schedule_scores_64() {
   __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);  // reads of LDS
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -764,7 +764,7 @@ __device__ __forceinline__ void many_body(const PagedAttendArgs& a, Job job, cha
     f32x16 S, S1;
     scores(from, here, S);
     scores(from, here + kBlock, S1);
-    if constexpr (D == 64 && QT == 1) schedule_scores();
+    if constexpr (D == 64 && QT == 1) schedule_scores_64();
     if (is.masked) {
       mask(S, s0, 0);
       mask(S1, s0, 1);
