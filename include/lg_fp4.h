@@ -92,7 +92,8 @@ size_t lg_paged_attend_fp4_workspace(const lg_paged_layer *layer, const lg_page_
  * those 32 values of out, whatever the slot's weight.
  *
  * Keys and values are exact as bfloat16, so the matrix products are of bfloat16 numbers with float32 sums: in float32
- * calls q and alpha are sums of three bfloat16 terms each, all of their 24 bits. In bfloat16 calls alpha is two terms (within 2^-16
+ * calls q and alpha are sums of three bfloat16 terms each, all of their 24 bits from 2^-110 on and what is not below 2^-133 of
+ * smaller ones (which count where keys or values reach 2^100). In bfloat16 calls alpha is two terms (within 2^-16
  * of it) where a sequence's new tokens have at most 32 query heads of a KV head together, and one (within 2^-8) in longer
  * chunks, as in lg_paged_attend. */
 lg_status lg_paged_attend_fp4(const lg_paged_layer *layer, const lg_page_map *map, lg_dtype dtype, const void *q,

@@ -556,3 +556,26 @@ def test_exponents_at_the_ends(dtype, D, n, keys, values):
                 assert (np.abs(out[row, heads] - o) <= tol).all(), (b, i, h, np.abs(out[row, heads] - o).max(), tol.min())
                 assert (np.abs(lse[row, heads] - ls) <= err + 2.0 ** -22 * (np.abs(ls) + big)).all(), (b, i, h)
                 assert (np.abs(sm[row, heads] - ms) <= 2 * err * ms + e * 2.0 ** -126).all(), (b, i, h)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n", [1, 40])
+@pytest.mark.parametrize("e", [60, 0, -60, -109, -110, -117])
+def test_bits_of_float32_queries(e, n, D):
+    """Each token sees its own slot alone and each query has one value, of 24 bits, where the key is one unit: the lse is the score,
+    one product. The terms of a query hold what is not below 2^-133, so the score is off by at most 2^-133 of the key (nothing
+    from 2^-110 on), by its scaling into and out of powers of two, four roundings of 2^-24, and by the log of a sum next to 1."""
+    a = Attend4(F32, D, 4, 1, 16, [0], [n], window=1, seed=30, holes=False)
+    at = a.r.randint(0, D, (a.T, 4))
+    m = (2 ** 23 + a.r.randint(0, 2 ** 23, (a.T, 4))) * a.r.choice([-1, 1], (a.T, 4)) * 2.0 ** (e - 23)
+    q = np.zeros((a.T, 4, D))
+    np.put_along_axis(q, at[..., None], m[..., None], -1)
+    a.q.copy_(torch.as_tensor(q.astype(np.float32)))
+    x = 127 - e + 6  # scores of 64 to 128 over sqrt(D)
+    block = fp4.pack(np.full(a.k.shape, 2, np.uint8), np.full((*a.k.shape[:-1], D // 32), x, np.uint8))
+    a.bytes[0].copy_(torch.as_tensor(block))
+    a.call()
+    s = m[:n] * 2.0 ** (x - 127) / np.sqrt(D)
+    lost = 2.0 ** -133 * 2.0 ** (x - 127) / np.sqrt(D) if e < -110 else 0
+    lse = a.results()[1][:n]
+    assert (np.abs(lse - s) <= 2.0 ** -21 * (np.abs(s) + 1) + lost).all(), np.abs(lse - s).max()
