@@ -8,14 +8,18 @@
 // queries and weights enter as three bfloat16 terms each (8 + 8 + 8 bits, exact), three times the instructions, still
 // a fifth of what float32 ones would take.
 //
-// What bounds it, measured on MI355X (a copy reaches 5.13 TB/s, a bfloat16 matrix product of 8192^3 1122 TFLOP/s), in a
-// graph: 64 sequences of 8192 slots, 32 / 8 heads of 128, 471 MB, 97 us, 4.85 TB/s: the memory. A decode step of 32 sequences of 28 / 4
-// heads and 1280 to 2047 slots, 30 MB, 14.4 us: its chain and its instructions. The sequence is known after 0.9 us, the first
+// What bounds it, measured on MI355X (a copy reaches 5.13 TB/s, plain reads 6.3 and non-temporal ones 7.0, a bfloat16 matrix product
+// of 8192^3 1122 TFLOP/s), in a graph: 64 sequences of 5120 to 8192 slots, 32 / 8 heads of 128, 471 MB, 97 us, 4.85 TB/s: loads
+// on their way, it seems, since neither the memory is at its reads' rate nor the vector instructions (49% of the cycles) or the
+// matrix ones (21%) are busy. A decode step of 32 sequences of 28 / 4
+// heads and 1280 to 2047 slots, 30 MB, 13.5 us: its chain and its instructions. The sequence is known after 0.9 us, the first
 // rows are asked for after 2.0, the first tile of 32 slots is done after 4.2, and each further one takes a wave 1.2 us beside
 // the others of its SIMD (230 vector and 16 matrix instructions, 100 scalar ones); the bytes alone would take 6. 4096 tokens of
-// 32 / 8 heads behind 4096, 412 GFLOP, 420 to 434 us, 950 to 980 TFLOP/s: matrix instructions, with the conversions and
-// exponentials beside them in part; in float32 1085 us, 380 TFLOP/s of exact products. Four sequences of 128 tokens with a window of
+// 32 / 8 heads behind 4096, 412 GFLOP, 419 us, 984 TFLOP/s: matrix instructions (42% of the cycles), with the conversions and
+// exponentials beside them in part (vector instructions 54%); at head_dim 64 267 us, 771 TFLOP/s, and the vector instructions
+// are first (70%, matrix ones 33%); in float32 1075 us, 384 TFLOP/s of exact products. Four sequences of 128 tokens with a window of
 // 2048 beside 12 that decode, 44 us: a workgroup's chain, 17 tiles of 2 us with one wave on a SIMD, and the launch that joins two splits.
+// 32 sequences of 5 tokens, 35 rows a KV head, 34 us: tiles of 128 rows, of which the last two waves have none.
 //
 // Tried and left (us, the decode step of 32 sequences / 64 sequences of 8192 slots unless said): tiles two to four ahead in
 // registers (16.7 to 17.6 against 15.8 / 103 to 109 against 97: the copies of their registers wait for all of them); the
@@ -1017,8 +1021,10 @@ constexpr long kFewSlots = 256;  // of a split at least: the launch that joins t
 constexpr long kManyTarget = 512;
 // Slots of a split there: 256, and one for every 32 query rows of the launch, whose partials are written and read.
 constexpr long kManySlots = 256, kRowsPerSlot = 32;
-// Slots of a split at most, whatever the number of workgroups: the capacity is all that the host knows, and one long sequence
-// among many short ones shall not hold up the launch.
+// A split for each whole 32768 slots at least (so one holds fewer than twice as many), whatever the number of workgroups: the
+// capacity is all that the host knows, and one long sequence among many short ones shall not hold up the launch. Beside a long
+// chunk a shorter one does: the splits go by the launch's workgroups, and a chunk of 4096 tokens behind 4096 with 8 sequences that
+// decode behind 32767 slots takes 667 us, in two calls 432 and 59.
 constexpr long kMaxSlots = 32768;
 constexpr long kMaxSplits = 64;
 // Rows that a launch joins at most: its 256 threads a workgroup of one row at least must stay below the 2^32 of a grid.

@@ -421,7 +421,8 @@ constexpr uint32_t kStays = 0xffffffffu;
 // the rows they fill, so what a pass writes in place no later pass reads, and fresh pages are nobody's
 // source). Where a row comes from and goes to takes two dependent loads (keep_idx, then the columns of both
 // ends), so a segment's rows look them up together and the passes find them in LDS, as slots of the pool (page x
-// page_size + row: below 2^32, since a slot has 128 bytes at least).
+// page_size + row: below 2^32, since a slot has 128 bytes at least and 2^32 of those fit no memory; 4-bit slots have fewer, and
+// check_paged_layer refuses pools of 2^32 - 1 of them).
 // Memory bounds it: 3.0 GB in 534 us, 5.6 TB/s, where a copy of 1 GiB runs at 5.2.
 //
 // 4-bit rows (L = 4 or 2 lanes of 16 bytes, in place of 8): an item is the whole row with its exponents, a byte a lane. The same
